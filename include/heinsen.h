@@ -48,13 +48,17 @@ enum {
                                      paragraph): re = log|x_t|, im = pi where x_t < 0, else 0; x_t = 0
                                      gives re = -inf.  Signs are always tracked (POSITIVE is ignored).
                                      Not available with LOG_INPUTS.                                     */
-    HEINSEN_LINEAR     = 1u << 6  /* comparison path: the same single-pass scan with the plain operator
+    HEINSEN_LINEAR     = 1u << 6, /* comparison path: the same single-pass scan with the plain operator
                                      (a1, b1) o (a2, b2) = (a1 a2, a2 b1 + b2) of the general formulation
                                      the paper compares itself with (Sec. 2), in float32, without any
                                      logarithm.  Partial products of a_t over up to a tile group of steps
                                      are formed, so they overflow or flush where the log-space form does
                                      not.  Excludes LOG_INPUTS, LOG_OUTPUT, OUT_COMPLEX; POSITIVE is
                                      ignored.                                                            */
+    /* Of the operators for language models below (refused by the scan entry points): */
+    HEINSEN_DECAY_PER_HEAD = 1u << 7, /* heinsen_linear_attention: log_a holds one value for each head   */
+    HEINSEN_GATE_SIGMOID   = 1u << 8  /* heinsen_block_norm: the gate's activation is sigmoid(x) instead of
+                                         x sigmoid(x)                                                    */
 };
 
 typedef enum {
@@ -236,6 +240,100 @@ int heinsen_set_timeline(void *stamps, uint64_t tiles);
  * Process-wide settings.  Every kernel still ends normally.  Returns a heinsen_status_t.
  */
 int heinsen_test_carry(uint32_t spin_limit, uint32_t drop_tile, uint32_t epoch, void *stream);
+
+/* ---- operators for language models -------------------------------------------------------------------------
+ *
+ * Linear attention with a decay for each head, the recurrence above with a matrix for a state, and the norms that
+ * stand around such a block.  Both are asynchronous on `stream`, take device pointers and return a heinsen_status_t
+ * as heinsen_scan does; nothing is launched where arguments are refused.  With HEINSEN_IN_BF16 the arrays named
+ * "stored" below are bfloat16, else float32.  Sums, states and statistics are float32 or wider throughout.
+ * Workspace: a grow-only buffer per (device, stream) apart from the scan's, under the same rules: allocated by the first
+ * call that needs it or needs more (HEINSEN_ERR_ALLOC), used as it is by a call recorded into a HIP graph
+ * (HEINSEN_ERR_UNSUPPORTED where an ordinary call of at least the same shape has not been made on that stream), freed by
+ * heinsen_release_scratch.  heinsen_block_norm and heinsen_linear_attention with n <= 4 need none.
+ * Results are bit-reproducible from run to run.
+ */
+
+/*
+ * heinsen_linear_attention -- for every sequence and head, over its tokens t = 1, 2, ...
+ *
+ *        S_t = a_t S_{t-1} + k_t v_t^T ,   a_t = exp(log_a_t)              (S: K x V)
+ *        o_t = scale * S_t^T q_t
+ *
+ *   q, k     : stored, [tokens, Hk, K]; tokens lie q_stride (k_stride) elements apart, heads of a token side by side.
+ *   v        : stored, [tokens, H, V], tokens v_stride elements apart.  A stride of 0 means contiguous tokens; larger ones
+ *              allow slices of a joint projection.  Head h of v goes with head h / (H / Hk) of q and k; H is a multiple of Hk.
+ *   log_a    : stored, [tokens, H], natural logarithms of the decays; [H] with HEINSEN_DECAY_PER_HEAD; NULL: a_t = 1.  Any
+ *              value is allowed; where exp(log_a) is zero in float32, -inf among them, the state starts afresh.
+ *   s0       : [B, H, K, V] float32, the states to start from; NULL: zeros.
+ *   out      : stored, [tokens, H, V], contiguous.
+ *   sn       : [B, H, K, V] float32, receives the states after the last tokens; NULL: not wanted.  May be s0.
+ *   starts   : NULL: B sequences of n tokens, one after the other.  Else device, B + 1 ascending int64: sequence b has the tokens
+ *              starts[b] .. starts[b + 1] - 1, and n is at least the length of the longest one (tokens past the n-th of a
+ *              sequence are left out).  A sequence without tokens hands its state on.
+ *   K, V     : 1 .. 128 (HEINSEN_ERR_UNSUPPORTED above).  Wider values are several heads that share q, k and log_a.
+ *
+ * Single tokens of a generating model are n = 1 with sn = s0.  n <= 4 goes token by token, which reads and writes the states
+ * once and little else; longer sequences go in chunks, those of few heads in segments side by side (workspace:
+ * 4 B H K V bytes for each segment).
+ * Products of bfloat16 arrays are exact and summed in float32; weights between tokens and the states are rounded to
+ * bfloat16 where they enter a product for out, never in the recurrence of the states itself.  float32 arrays are
+ * multiplied in float32.  Other sequences and heads, and tokens before it, never see an infinite or NaN value.
+ */
+int heinsen_linear_attention(const void *q, const void *k, const void *v, const void *log_a, const void *s0, void *out, void *sn,
+                             const void *starts, int64_t B, int64_t n, int64_t H, int64_t Hk, int64_t K, int64_t V,
+                             int64_t q_stride, int64_t k_stride, int64_t v_stride, float scale, uint32_t flags, void *stream);
+
+/*
+ * heinsen_linear_attention_backward -- gradients of a loss with respect to every input of heinsen_linear_attention, whose
+ * arguments are those of that call.
+ *   grad_out   : stored, [tokens, H, V], contiguous.       grad_sn: [B, H, K, V] float32; NULL: zeros.
+ *   grad_q, grad_k : stored, [tokens, Hk, K], contiguous; where heads of v share them, the sum over these.
+ *   grad_v     : stored, [tokens, H, V], contiguous.
+ *   grad_log_a : stored, [tokens, H], or [H] with HEINSEN_DECAY_PER_HEAD (the sum over all tokens); may be NULL.
+ *   grad_s0    : [B, H, K, V] float32; may be NULL.
+ * Nothing of the forward call is needed.  Workspace: the states at the chunks' starts (64 tokens in bfloat16, 32 in float32),
+ * stored, K and V rounded up to 64 or 128, B * ceil(n / chunk) of them for each head; with shared heads 8 K more bytes for each
+ * of B n H tokens and heads.  An infinite or NaN value reaches the gradients of its own sequence and head only, those
+ * of earlier tokens among them.
+ */
+int heinsen_linear_attention_backward(const void *q, const void *k, const void *v, const void *log_a, const void *s0,
+                                      const void *grad_out, const void *grad_sn, void *grad_q, void *grad_k, void *grad_v,
+                                      void *grad_log_a, void *grad_s0, const void *starts, int64_t B, int64_t n, int64_t H,
+                                      int64_t Hk, int64_t K, int64_t V, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                      float scale, uint32_t flags, void *stream);
+
+/*
+ * heinsen_block_norm -- the norm after a block, its gate, residual scale and residual, and the norm before the next block,
+ * for each of `rows` rows of D entries:
+ *
+ *        z = u / sqrt(mean(u^2) + eps) * w_post          (w_post NULL: z = u)
+ *        h = residual + scale * (act(gate) * z)          act(x) = x sigmoid(x), sigmoid(x) with HEINSEN_GATE_SIGMOID
+ *        y = h / sqrt(mean(h^2) + eps) * w_pre
+ *
+ *   u, gate, residual : stored, [rows, D]; rows of u and gate lie u_stride and gate_stride elements apart (0: D).  gate NULL:
+ *                       no gate; residual NULL: none is added.
+ *   scale, w_post, w_pre : [D] float32; scale NULL: 1.
+ *   h, y     : stored, [rows, D], contiguous.  Either may be NULL; y needs w_pre.  Each may be an input array of the same
+ *              layout.  y is formed from h before it is rounded.
+ *   D        : 1 .. HEINSEN_NORM_MAX_D (HEINSEN_ERR_UNSUPPORTED above).
+ * The norm of each head of an attention, gated, is a call with rows = tokens * heads and neither residual nor y.
+ */
+#define HEINSEN_NORM_MAX_D 16384
+int heinsen_block_norm(const void *u, const void *gate, const void *residual, const void *scale, const void *w_post,
+                       const void *w_pre, void *h, void *y, int64_t rows, int64_t D, int64_t u_stride, int64_t gate_stride,
+                       float eps, uint32_t flags, void *stream);
+
+/*
+ * heinsen_block_norm_backward -- gradients with respect to every input of heinsen_block_norm, whose arguments are those of
+ * that call.  grad_h, grad_y: stored, [rows, D], contiguous; one of the two may be NULL (zeros).  grad_u, grad_gate,
+ * grad_residual: stored, [rows, D], contiguous; grad_scale, grad_w_post, grad_w_pre: [D] float32, sums over the rows in a
+ * fixed order.  All but grad_u may be NULL.  Gradients of rows may be written over grad_h or grad_y.
+ */
+int heinsen_block_norm_backward(const void *u, const void *gate, const void *residual, const void *scale, const void *w_post,
+                                const void *w_pre, const void *grad_h, const void *grad_y, void *grad_u, void *grad_gate,
+                                void *grad_residual, void *grad_scale, void *grad_w_post, void *grad_w_pre, int64_t rows,
+                                int64_t D, int64_t u_stride, int64_t gate_stride, float eps, uint32_t flags, void *stream);
 
 #ifdef __cplusplus
 }

@@ -25,9 +25,11 @@ HEINSEN_POSITIVE = 1 << 3
 HEINSEN_X0_SCALAR = 1 << 4
 HEINSEN_OUT_COMPLEX = 1 << 5
 HEINSEN_LINEAR = 1 << 6
+HEINSEN_DECAY_PER_HEAD = 1 << 7
+HEINSEN_GATE_SIGMOID = 1 << 8
 FLAGS = {"LOG_INPUTS": HEINSEN_LOG_INPUTS, "LOG_OUTPUT": HEINSEN_LOG_OUTPUT, "IN_BF16": HEINSEN_IN_BF16,
          "POSITIVE": HEINSEN_POSITIVE, "X0_SCALAR": HEINSEN_X0_SCALAR, "OUT_COMPLEX": HEINSEN_OUT_COMPLEX,
-         "LINEAR": HEINSEN_LINEAR}
+         "LINEAR": HEINSEN_LINEAR, "DECAY_PER_HEAD": HEINSEN_DECAY_PER_HEAD, "GATE_SIGMOID": HEINSEN_GATE_SIGMOID}
 
 HEINSEN_OK = 0
 HEINSEN_ERR_INVALID_ARG = 1
@@ -39,7 +41,8 @@ HEINSEN_ERR_CARRY_LOST = 6
 
 EXPORTS = ("heinsen_scan", "heinsen_scan_static", "heinsen_status_string", "heinsen_last_hip_error", "heinsen_version",
            "heinsen_release_scratch", "heinsen_kernel_name", "heinsen_tile_shape", "heinsen_sequential", "heinsen_check",
-           "heinsen_set_timeline", "heinsen_test_carry", "heinsen_stream_probe")
+           "heinsen_set_timeline", "heinsen_test_carry", "heinsen_stream_probe", "heinsen_linear_attention",
+           "heinsen_linear_attention_backward", "heinsen_block_norm", "heinsen_block_norm_backward")
 
 _lib = None
 _call = None  # the scan entry points without ctypes (csrc/call.c), once the library is loaded
@@ -100,6 +103,15 @@ def _open():
     lib.heinsen_stream_probe.restype = ci
     lib.heinsen_sequential.argtypes = [vp, vp, vp, vp, i64, vp]
     lib.heinsen_sequential.restype = ci
+    f32 = ctypes.c_float
+    lib.heinsen_linear_attention.argtypes = [vp] * 8 + [i64] * 9 + [f32, u32, vp]
+    lib.heinsen_linear_attention.restype = ci
+    lib.heinsen_linear_attention_backward.argtypes = [vp] * 13 + [i64] * 9 + [f32, u32, vp]
+    lib.heinsen_linear_attention_backward.restype = ci
+    lib.heinsen_block_norm.argtypes = [vp] * 8 + [i64] * 4 + [f32, u32, vp]
+    lib.heinsen_block_norm.restype = ci
+    lib.heinsen_block_norm_backward.argtypes = [vp] * 14 + [i64] * 4 + [f32, u32, vp]
+    lib.heinsen_block_norm_backward.restype = ci
     call.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.heinsen_scan, lib.heinsen_scan_static)))
     return lib, call
 
@@ -263,3 +275,51 @@ def heinsen_sequential(a, b, x0, out, n: int, stream=None) -> None:
     st = int(load().heinsen_sequential(_addr(a), _addr(b), _addr(x0), _addr(out), int(n), _stream_handle(stream)))
     if st != HEINSEN_OK:
         raise HeinsenError(st, heinsen_status_string(st))
+
+
+def _raise_for(st: int) -> None:
+    if st != HEINSEN_OK:
+        msg = heinsen_status_string(st)
+        if st in (HEINSEN_ERR_HIP, HEINSEN_ERR_ALLOC):
+            msg += f", hipError_t {heinsen_last_hip_error()}"
+        raise HeinsenError(st, msg)
+
+
+def heinsen_linear_attention(q, k, v, log_a, s0, out, sn, B: int, n: int, H: int, K: int, V: int, scale: float, flags: int, stream=None, *,
+                             Hk=None, starts=None, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> None:
+    """S_t = a_t S_{t-1} + k_t v_t^T, out_t = scale S_t^T q_t for B sequences of up to n tokens and H heads; see
+    include/heinsen.h.  Asynchronous on `stream`.
+
+    Hk: heads of q and k (default: H).  starts: device int64 [B + 1], where sequences of different lengths start."""
+    _raise_for(load().heinsen_linear_attention(
+        _addr(q), _addr(k), _addr(v), _addr(log_a), _addr(s0), _addr(out), _addr(sn), _addr(starts), int(B), int(n), int(H),
+        int(H if Hk is None else Hk), int(K), int(V), int(q_stride), int(k_stride), int(v_stride), scale, int(flags), _stream_handle(stream)))
+
+
+def heinsen_linear_attention_backward(q, k, v, log_a, s0, grad_out, grad_sn, grad_q, grad_k, grad_v, grad_log_a, grad_s0, B: int, n: int,
+                                      H: int, K: int, V: int, scale: float, flags: int, stream=None, *, Hk=None, starts=None,
+                                      q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> None:
+    """Gradients of heinsen_linear_attention; see include/heinsen.h.  grad_sn, grad_log_a and grad_s0 may be None."""
+    _raise_for(load().heinsen_linear_attention_backward(
+        _addr(q), _addr(k), _addr(v), _addr(log_a), _addr(s0), _addr(grad_out), _addr(grad_sn), _addr(grad_q), _addr(grad_k), _addr(grad_v),
+        _addr(grad_log_a), _addr(grad_s0), _addr(starts), int(B), int(n), int(H), int(H if Hk is None else Hk), int(K), int(V),
+        int(q_stride), int(k_stride), int(v_stride), scale, int(flags), _stream_handle(stream)))
+
+
+def heinsen_block_norm(u, gate, residual, scale, w_post, w_pre, h, y, rows: int, D: int, eps: float, flags: int, stream=None, *,
+                       u_stride: int = 0, gate_stride: int = 0) -> None:
+    """h = residual + scale * act(gate) * norm(u) w_post, y = norm(h) w_pre; see include/heinsen.h.  Arguments that are not
+    wanted are None."""
+    _raise_for(load().heinsen_block_norm(
+        _addr(u), _addr(gate), _addr(residual), _addr(scale), _addr(w_post), _addr(w_pre), _addr(h), _addr(y), int(rows), int(D),
+        int(u_stride), int(gate_stride), eps, int(flags), _stream_handle(stream)))
+
+
+def heinsen_block_norm_backward(u, gate, residual, scale, w_post, w_pre, grad_h, grad_y, grad_u, grad_gate, grad_residual, grad_scale,
+                                grad_w_post, grad_w_pre, rows: int, D: int, eps: float, flags: int, stream=None, *, u_stride: int = 0,
+                                gate_stride: int = 0) -> None:
+    """Gradients of heinsen_block_norm; see include/heinsen.h.  All gradients but grad_u may be None."""
+    _raise_for(load().heinsen_block_norm_backward(
+        _addr(u), _addr(gate), _addr(residual), _addr(scale), _addr(w_post), _addr(w_pre), _addr(grad_h), _addr(grad_y), _addr(grad_u),
+        _addr(grad_gate), _addr(grad_residual), _addr(grad_scale), _addr(grad_w_post), _addr(grad_w_pre), int(rows), int(D), int(u_stride),
+        int(gate_stride), eps, int(flags), _stream_handle(stream)))

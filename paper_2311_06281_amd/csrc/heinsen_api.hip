@@ -1,6 +1,7 @@
 // C ABI of libheinsen: argument validation, scratch cache, dispatch to the two layout paths.
 #include "../../include/heinsen.h"
 #include "heinsen_internal.hpp"
+#include "operators.hpp"
 
 #include <cstdio>
 #include <cstring>
@@ -174,12 +175,6 @@ hs::LaunchCtx make_ctx(unsigned long long *records)
     return hs::LaunchCtx{records, g_spin_limit, g_drop_tile, g_timeline, g_timeline_tiles};
 }
 
-bool is_capturing(hipStream_t stream)
-{
-    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-    return stream != nullptr && hipStreamIsCapturing(stream, &cap) == hipSuccess && cap != hipStreamCaptureStatusNone;
-}
-
 // Checks the arguments of a scan call and fills `c`; `bnd` tells which layout path serves it.
 int make_call(const void *a, const void *b, const void *x0, void *out, int64_t B, int64_t D, int64_t n, int layout,
               uint32_t flags, void *stream, hs::ScanCall &c, bool &bnd)
@@ -201,6 +196,18 @@ int make_call(const void *a, const void *b, const void *x0, void *out, int64_t B
 
 } // namespace
 
+namespace hs {
+
+bool note_hip(hipError_t e) { return hip_ok(e); }
+
+bool is_capturing(hipStream_t stream)
+{
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    return stream != nullptr && hipStreamIsCapturing(stream, &cap) == hipSuccess && cap != hipStreamCaptureStatusNone;
+}
+
+} // namespace hs
+
 extern "C" {
 
 int heinsen_scan(const void *a, const void *b, const void *x0, void *out, int64_t B, int64_t D, int64_t n,
@@ -219,7 +226,7 @@ int heinsen_scan(const void *a, const void *b, const void *x0, void *out, int64_
         // allocate: it uses the buffer the stream already has.  Nothing else is special about it -- the
         // kernels keep tickets and launch counter in the buffer themselves.
         Scratch *sc = nullptr;
-        st = ensure_scratch(c.stream, hs::kRecordBase + need.records, is_capturing(c.stream), sc);
+        st = ensure_scratch(c.stream, hs::kRecordBase + need.records, hs::is_capturing(c.stream), sc);
         if (st != HEINSEN_OK) return st;
         records = sc->records;
     }
@@ -243,7 +250,7 @@ int heinsen_scan_static(const void *a, const void *b, const void *x0, void *out,
     if (need.records != 0) {
         // The array keeps whatever the last call left in it.  Nothing has to be cleared: every launch finds
         // in the header a launch counter that no record in the array carries yet.
-        st = static_scratch(c.stream, is_capturing(c.stream), records);
+        st = static_scratch(c.stream, hs::is_capturing(c.stream), records);
         if (st != HEINSEN_OK) return st;
     }
     const hs::LaunchCtx ctx = make_ctx(records);
@@ -329,7 +336,7 @@ const char *heinsen_status_string(int status)
 
 int heinsen_last_hip_error(void) { return t_last_hip_error; }
 
-int heinsen_version(void) { return 301; /* 0.3.1: 0.3.0 (heinsen_scan_static, heinsen_check, heinsen_set_timeline) + heinsen_tile_shape */ }
+int heinsen_version(void) { return 400; /* 0.4.0: + heinsen_linear_attention, heinsen_block_norm and their gradients */ }
 
 int heinsen_release_scratch(void)
 {
@@ -347,6 +354,7 @@ int heinsen_release_scratch(void)
         for (unsigned long long *old : kv.second.retired) (void)hipFree(old);
     }
     g_scratch.clear();
+    if (hs::release_workspaces() != HEINSEN_OK) status = HEINSEN_ERR_HIP;
     if (have_prev) (void)hipSetDevice(prev);
     return status;
 }

@@ -1,0 +1,561 @@
+// Gradients of linear attention with a decay for each head.
+//
+// With R_t the gradient of the state S_t (R_t = a_{t+1} R_{t+1} + scale q_t do_t^T, plus that of the final state at the end),
+//     dq_t = scale S_t do_t,  dk_t = R_t v_t,  dv_t = R_t^T k_t,  dlog a_t = <R_t, a_t S_{t-1}>,  dS_0 = a_1 R_1.
+// In a chunk of C tokens, with S the state at its start, R the gradient of the state at its end, and for s <= t
+// P_ts = scale e^{G_t-G_s} q_t . k_s and D_ts = scale e^{G_t-G_s} do_t . v_s:
+//     dq_t = sum_s D_ts k_s + scale e^{G_t} S do_t          (x_t: q_t . the second term)
+//     dk_s = sum_t D_ts q_t + e^{G_C-G_s} R v_s             (y_s: k_s . the second term)
+//     dv_s = sum_t P_ts do_t + e^{G_C-G_s} R^T k_s
+//     R'   = e^{G_C} R + sum_t scale e^{G_t} q_t do_t^T
+//     dlog a_u = sum_{t>=u} x_t + sum_{s<u} y_s + e^{G_C} <R, S> + sum_{t>=u>s} P_ts (do_t . v_s)
+// The last line follows what a decay spans: pairs of a token after it and one before it, both in the chunk, one or none.
+// (Sums of q . dq - k . dk over the tokens after it are the same number, but there the pairs that it does not span have to
+// cancel, and the rounding of the operands would not.)
+#include "attention_tiles.hpp"
+#include "operators.hpp"
+
+namespace hs {
+namespace {
+
+struct BackwardArgs {
+    const void *q, *k, *v, *log_a, *grad_out;
+    const float *grad_sn;
+    const int64_t *starts;
+    const void *states;           // [B, H, chunks, DK, DV] in T: the state at each chunk's start
+    const float *segment_grad;    // [B, H, segments, K, V]: where there are several, the gradient of the state at each one's end
+    void *grad_q, *grad_k;        // T, or float for each head of v where heads share q and k
+    void *grad_v, *grad_log_a;    // grad_log_a: T, or float [tokens, H] with per_head, or null
+    float *grad_s0;
+    int64_t n, q_stride, k_stride, v_stride, segment;
+    int H, share, K, V, segments, chunks;
+    float scale;
+    bool per_head, q_whole, k_whole, v_whole, out_whole, grad_qk_whole, grad_v_whole;
+};
+
+// A workgroup takes one segment of one head's tokens from its last chunk to its first; the gradient R of the state is in
+// registers, 16 columns to a wave.
+template <typename T, int C, int DK, int DV>
+__global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(BackwardArgs p)
+{
+    constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
+    constexpr int PK = pitch<T>(DK), PV = pitch<T>(DV), PP = pitch<T>(C);
+    constexpr int PLANES = sizeof(T) == 4 ? 1 : 3; // of q do^T's operand, see heinsen_attention_sweep
+    __shared__ __align__(16) T qs[C * PK];
+    __shared__ __align__(16) T ks[C * PK];
+    __shared__ __align__(16) T vs[C * PV];
+    __shared__ __align__(16) T os[C * PV];  // grad_out
+    __shared__ __align__(16) T rs[DV * PK]; // R transposed
+    __shared__ __align__(16) T ps[C * PP];  // P transposed: [s][t]
+    __shared__ __align__(16) T ds[C * PP];  // D transposed
+    __shared__ Decays<C> decays;
+    __shared__ float xs[KT][C], ys[KT][C], pair_rows[TT][C], pair_cols[TT][C], spans[WAVES];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    const int seg = blockIdx.x % p.segments, bh = blockIdx.x / p.segments, h = bh % p.H, b = bh / p.H;
+    int64_t first;
+    const int64_t len = sequence(p.starts, p.n, b, first);
+    const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
+    if (begin >= len && seg > 0) return;
+
+    const T *const q = static_cast<const T *>(p.q) + first * p.q_stride + (int64_t)(h / p.share) * p.K;
+    const T *const k = static_cast<const T *>(p.k) + first * p.k_stride + (int64_t)(h / p.share) * p.K;
+    const T *const v = static_cast<const T *>(p.v) + first * p.v_stride + (int64_t)h * p.V;
+    const T *const o = static_cast<const T *>(p.grad_out) + (first * p.H + h) * p.V;
+    const T *const log_a = static_cast<const T *>(p.log_a);
+    const int64_t o_stride = (int64_t)p.H * p.V;
+
+    const int col = wave * 16 + r;
+    f32x4 grad[KT]; // R
+    const float *const from = p.segments > 1 && begin < len ? p.segment_grad + ((int64_t)bh * p.segments + seg) * p.K * p.V
+                              : p.grad_sn ? p.grad_sn + (int64_t)bh * p.K * p.V : nullptr;
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = 16 * i + 4 * g + e;
+            grad[i][e] = from && row < p.K && col < p.V ? from[(int64_t)row * p.V + col] : 0.0f;
+        }
+
+    const int chunks = (int)((end - begin + C - 1) / C);
+    TileLoad<T, C, DK, THREADS> next_q, next_k;
+    TileLoad<T, C, DV, THREADS> next_v, next_o;
+    float next_log_a = 0.0f;
+    auto request = [&](int64_t t0) {
+        const int rows = (int)(end - t0 < C ? end - t0 : C);
+        next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K, p.q_whole);
+        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K, p.k_whole);
+        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, p.V, p.v_whole);
+        next_o.load(o + t0 * o_stride, o_stride, rows, p.V, p.out_whole);
+        if (wave == 0)
+            next_log_a = log_a == nullptr || lane >= rows ? 0.0f
+                         : p.per_head ? to_float(log_a[h]) : to_float(log_a[(first + t0 + lane) * p.H + h]);
+    };
+    if (chunks > 0) request(begin + (int64_t)(chunks - 1) * C);
+
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+        const int64_t t0 = begin + (int64_t)chunk * C;
+        const int rows = (int)(end - t0 < C ? end - t0 : C);
+        next_q.store(qs);
+        next_k.store(ks);
+        next_v.store(vs);
+        next_o.store(os);
+        if (wave == 0) write_decays<C>(decays, next_log_a, lane);
+#pragma unroll
+        for (int i = 0; i < KT; ++i) *reinterpret_cast<x4<T> *>(rs + col * PK + 16 * i + 4 * g) = __builtin_convertvector(grad[i], x4<T>);
+        __syncthreads();
+        if (chunk > 0) request(t0 - C);
+        const T *const state = static_cast<const T *>(p.states) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV);
+
+        // P, D and the pairs' sums, in tiles of 16 x 16 on and below the diagonal, and zeros beside it where a product
+        // takes two tiles at a time
+        for (int at = wave; at < TT * TT; at += WAVES) {
+            const int tt = at / TT, st = at % TT;
+            if (st > (tt | 1)) continue;
+            f32x4 pt = {0, 0, 0, 0}, dt = {0, 0, 0, 0};
+            if (st <= tt) {
+#pragma unroll
+                for (int i = 0; i < DK / 32; ++i) pt = mma(load_rows(qs, PK, 16 * tt, 32 * i, lane), load_rows(ks, PK, 16 * st, 32 * i, lane), pt);
+#pragma unroll
+                for (int i = 0; i < DV / 32; ++i) dt = mma(load_rows(os, PV, 16 * tt, 32 * i, lane), load_rows(vs, PV, 16 * st, 32 * i, lane), dt);
+                const int s = 16 * st + r; // rows: tokens t, columns: tokens s
+                const float whole_s = decays.whole[s], part_s = decays.part[s];
+                float below = 0.0f;
+                f32x4 across;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = 16 * tt + 4 * g + e;
+                    const float w = __builtin_amdgcn_exp2f((decays.whole[t] - whole_s) + (decays.part[t] - part_s)) * p.scale;
+                    const float pair = s < t ? pt[e] * w * dt[e] : 0.0f;
+                    below += pair;
+                    across[e] = pair;
+                    pt[e] = s <= t ? pt[e] * w : 0.0f;
+                    dt[e] = s <= t ? dt[e] * w : 0.0f;
+                }
+                below += __shfl_xor(below, 16);
+                below += __shfl_xor(below, 32);
+                if (g == 0) pair_cols[tt][s] = below;
+#pragma unroll
+                for (int by = 1; by < 16; by *= 2)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) across[e] += __shfl_xor(across[e], by);
+                if (r == 0) *reinterpret_cast<f32x4 *>(&pair_rows[st][16 * tt + 4 * g]) = across;
+            }
+            *reinterpret_cast<x4<T> *>(ps + (16 * st + r) * PP + 16 * tt + 4 * g) = __builtin_convertvector(pt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ds + (16 * st + r) * PP + 16 * tt + 4 * g) = __builtin_convertvector(dt, x4<T>);
+        }
+        __syncthreads();
+
+        // dv, rows: this wave's columns of v, columns: tokens s
+        {
+            Frag<T> rf[DK / 32];
+#pragma unroll
+            for (int i = 0; i < DK / 32; ++i) rf[i] = to_frag<T>(grad[2 * i], grad[2 * i + 1]);
+#pragma unroll
+            for (int st = 0; st < TT; ++st) {
+                f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < DK / 32; ++i) acc = mma(rf[i], load_rows(ks, PK, 16 * st, 32 * i, lane), acc);
+                acc *= decays.to_end[16 * st + r];
+#pragma unroll
+                for (int i = st / 2; i < C / 32; ++i)
+                    acc = mma(load_cols(os, PV, 16 * wave, 32 * i, lane), load_rows(ps, PP, 16 * st, 32 * i, lane), acc);
+                if (16 * st + r < rows)
+                    store4(static_cast<T *>(p.grad_v) + ((first + t0 + 16 * st + r) * p.H + h) * (int64_t)p.V, 16 * wave + 4 * g, p.V,
+                           p.grad_v_whole, acc);
+            }
+        }
+        // dq and dk: 16 columns of q and k at a time, tokens in the columns
+        for (int kt = wave % KT; kt < KT; kt += WAVES) {
+            Frag<T> sf[DV / 32], rf[DV / 32];
+#pragma unroll
+            for (int i = 0; i < DV / 32; ++i) {
+                const T *const at = state + (16 * kt + r) * DV + 32 * i + 4 * g;
+                sf[i] = join<T>(*reinterpret_cast<const x4<T> *>(at), *reinterpret_cast<const x4<T> *>(at + 16));
+                rf[i] = load_cols(rs, PK, 16 * kt, 32 * i, lane);
+            }
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                if (WAVES > KT && (t % (WAVES / KT > 0 ? WAVES / KT : 1)) != wave / KT) continue;
+                const int token = 16 * t + r;
+                f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < DV / 32; ++i) acc = mma(sf[i], load_rows(os, PV, 16 * t, 32 * i, lane), acc);
+                acc *= decays.from_start[token] * p.scale;
+                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + token * PK + 16 * kt + 4 * g);
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (g == 0) xs[kt][token] = sum;
+#pragma unroll
+                for (int i = 0; i <= t / 2; ++i)
+                    acc = mma(load_cols(ks, PK, 16 * kt, 32 * i, lane), load_cols(ds, PP, 16 * t, 32 * i, lane), acc);
+                // a head of v's own part of a shared gradient goes to the scratch, n places for each sequence
+                const int64_t place = (p.share > 1 ? b * p.n : first) + t0 + token;
+                if (token < rows) {
+                    if (p.share > 1) store4(static_cast<float *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
+                    else store4(static_cast<T *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
+                }
+
+                acc = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < DV / 32; ++i) acc = mma(rf[i], load_rows(vs, PV, 16 * t, 32 * i, lane), acc);
+                acc *= decays.to_end[token];
+                own = *reinterpret_cast<const x4<T> *>(ks + token * PK + 16 * kt + 4 * g);
+                sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (g == 0) ys[kt][token] = sum;
+#pragma unroll
+                for (int i = t / 2; i < C / 32; ++i)
+                    acc = mma(load_cols(qs, PK, 16 * kt, 32 * i, lane), load_rows(ds, PP, 16 * t, 32 * i, lane), acc);
+                if (token < rows) {
+                    if (p.share > 1) store4(static_cast<float *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
+                    else store4(static_cast<T *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
+                }
+            }
+        }
+        // <R, S>, and R at the chunk's start
+        {
+            const float decay = decays.total;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < KT; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += grad[i][e] * to_float(state[(16 * i + 4 * g + e) * DV + col]);
+                grad[i] *= decay;
+            }
+#pragma unroll
+            for (int by = 1; by < 64; by *= 2) sum += __shfl_xor(sum, by);
+            if (lane == 0) spans[wave] = sum * decay;
+#pragma unroll
+            for (int i = 0; i < C / 32; ++i) {
+                const Frag<T> of = load_cols(os, PV, 16 * wave, 32 * i, lane);
+                Frag<T> planes[PLANES];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float x = to_float(of[e]) * (decays.from_start[32 * i + 4 * g + (e >> 2) * 16 + (e & 3)] * p.scale);
+#pragma unroll
+                    for (int j = 0; j < PLANES; ++j) {
+                        planes[j][e] = (T)x;
+                        x -= to_float(planes[j][e]);
+                    }
+                }
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const Frag<T> qf = load_cols(qs, PK, 16 * kt, 32 * i, lane);
+#pragma unroll
+                    for (int j = 0; j < PLANES; ++j) grad[kt] = mma(qf, planes[j], grad[kt]);
+                }
+            }
+        }
+        __syncthreads();
+        if (wave == 0 && p.grad_log_a) { // before the next chunk's sums are written there is another barrier
+            double suffix = 0.0, prefix = 0.0, span = 0.0;
+            if (lane < C) {
+                float x = 0.0f, y = 0.0f, across = 0.0f, below = 0.0f;
+#pragma unroll
+                for (int i = 0; i < KT; ++i) x += xs[i][lane], y += ys[i][lane];
+                for (int i = 0; i < TT; ++i) {
+                    if (i <= lane / 16) across += pair_rows[i][lane];
+                    if (i >= lane / 16) below += pair_cols[i][lane];
+                }
+                suffix = (double)x + ((double)across - (double)below), prefix = y;
+            }
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) span += spans[i];
+            const double own = prefix;
+#pragma unroll
+            for (int by = 1; by < C; by *= 2) {
+                const double up = lane_up(prefix, by), down = lane_at(suffix, (lane + by) & 63);
+                if (lane >= by) prefix += up;
+                if (lane + by < C) suffix += down;
+            }
+            if (lane < rows) {
+                const float sum = (float)(suffix + (prefix - own) + span);
+                if (p.per_head) static_cast<float *>(p.grad_log_a)[(b * p.n + t0 + lane) * p.H + h] = sum;
+                else static_cast<T *>(p.grad_log_a)[(first + t0 + lane) * p.H + h] = (T)sum;
+            }
+        }
+    }
+
+    if (p.grad_s0 && seg == 0) {
+        float *const to = p.grad_s0 + (int64_t)bh * p.K * p.V;
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = 16 * i + 4 * g + e;
+                if (row < p.K && col < p.V) to[(int64_t)row * p.V + col] = grad[i][e];
+            }
+    }
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------------
+//
+// The recurrence and its gradients token by token in float32: s0 and grad_sn are read once, the states in between are formed
+// again for each token.  A workgroup has a head's state; a thread has VEC neighbouring columns of every ROWS-th row.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardArgs p, const float *s0)
+{
+    constexpr int ACROSS = 128 / VEC, ROWS = 256 / ACROSS, PER = 128 / ROWS, IN_WAVE = ACROSS < 64 ? ACROSS : 64, PARTS = ACROSS / IN_WAVE;
+    typedef float vec __attribute__((ext_vector_type(VEC)));
+    __shared__ float q[kFewTokens][128], k[kFewTokens][128], v[kFewTokens][128], o[kFewTokens][128], a[kFewTokens];
+    __shared__ float row_sums[2][PARTS][128], col_sums[ROWS][128], wave_sums[4];
+    const int bh = blockIdx.x, h = bh % p.H, b = bh / p.H;
+    const int row0 = threadIdx.x / ACROSS, col = threadIdx.x % ACROSS * VEC, part = threadIdx.x % ACROSS / IN_WAVE;
+    const bool inside = col < p.V;
+    int64_t first;
+    const int len = (int)sequence(p.starts, p.n, b, first);
+    const int64_t at = (int64_t)bh * p.K * p.V + col;
+
+    vec start[PER], grad[PER]; // s0 and R
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int row = row0 + i * ROWS;
+        start[i] = grad[i] = (vec)0.0f;
+        if (s0 && inside && row < p.K) start[i] = *reinterpret_cast<const vec *>(s0 + at + (int64_t)row * p.V);
+        if (p.grad_sn && inside && row < p.K) grad[i] = *reinterpret_cast<const vec *>(p.grad_sn + at + (int64_t)row * p.V);
+    }
+    for (int i = threadIdx.x; i < len * 128; i += 256) {
+        const int t = i / 128, c = i % 128;
+        const int64_t token = first + t, qk = (int64_t)(h / p.share) * p.K + c, value = (int64_t)h * p.V + c;
+        q[t][c] = c < p.K ? to_float(static_cast<const T *>(p.q)[token * p.q_stride + qk]) * p.scale : 0.0f;
+        k[t][c] = c < p.K ? to_float(static_cast<const T *>(p.k)[token * p.k_stride + qk]) : 0.0f;
+        v[t][c] = c < p.V ? to_float(static_cast<const T *>(p.v)[token * p.v_stride + value]) : 0.0f;
+        o[t][c] = c < p.V ? to_float(static_cast<const T *>(p.grad_out)[token * p.H * p.V + value]) : 0.0f;
+        if (c == 0) {
+            const T *const log_a = static_cast<const T *>(p.log_a);
+            const float la = log_a == nullptr ? 0.0f : to_float(log_a[p.per_head ? h : token * p.H + h]);
+            a[t] = la <= -104.0f ? 0.0f : expf(la);
+        }
+    }
+    __syncthreads();
+    auto values = [&](const float *x) {
+        vec e;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) e[i] = x[col + i];
+        return e;
+    };
+    for (int t = len - 1; t >= 0; --t) {
+        const vec vt = values(v[t]), ot = values(o[t]);
+        vec down = (vec)0.0f;
+        float span = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int row = row0 + i * ROWS;
+            vec s = start[i];
+            for (int u = 0; u < t; ++u) s = s * a[u] + k[u][row] * values(v[u]);
+            grad[i] += q[t][row] * ot;
+            vec dq = grad[i] * s, dk = grad[i] * vt;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) span += dq[e];
+            s = s * a[t] + k[t][row] * vt;
+            dq = s * ot;
+            down += k[t][row] * grad[i];
+            float sum_q = 0.0f, sum_k = 0.0f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum_q += dq[e], sum_k += dk[e];
+#pragma unroll
+            for (int by = 1; by < IN_WAVE; by *= 2) sum_q += __shfl_xor(sum_q, by), sum_k += __shfl_xor(sum_k, by);
+            if (threadIdx.x % IN_WAVE == 0) row_sums[0][part][row] = sum_q, row_sums[1][part][row] = sum_k;
+            grad[i] *= a[t];
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) col_sums[row0][col + e] = down[e];
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) span += __shfl_xor(span, by);
+        if (threadIdx.x % 64 == 0) wave_sums[threadIdx.x / 64] = span;
+        __syncthreads();
+        const int c = threadIdx.x & 127;
+        const int64_t token = first + t, place = ((p.share > 1 ? (int64_t)b * p.n + t : token) * p.H + h) * p.K + c;
+        if (c < p.K) {
+            const int which = threadIdx.x / 128;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) sum += row_sums[which][i][c];
+            if (which == 0) sum *= p.scale;
+            void *const to = which == 0 ? p.grad_q : p.grad_k;
+            if (p.share > 1) static_cast<float *>(to)[place] = sum;
+            else static_cast<T *>(to)[place] = (T)sum;
+        }
+        if (threadIdx.x < p.V) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) sum += col_sums[i][threadIdx.x];
+            static_cast<T *>(p.grad_v)[(token * p.H + h) * p.V + threadIdx.x] = (T)sum;
+        }
+        if (threadIdx.x == 0 && p.grad_log_a) {
+            const float sum = a[t] * ((wave_sums[0] + wave_sums[1]) + (wave_sums[2] + wave_sums[3]));
+            if (p.per_head) static_cast<float *>(p.grad_log_a)[(b * p.n + t) * p.H + h] = sum;
+            else static_cast<T *>(p.grad_log_a)[token * p.H + h] = (T)sum;
+        }
+        __syncthreads();
+    }
+    if (p.grad_s0 && inside)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int row = row0 + i * ROWS;
+            if (row < p.K) *reinterpret_cast<vec *>(p.grad_s0 + at + (int64_t)row * p.V) = grad[i];
+        }
+}
+
+// Gradients of shared q and k: the sum over the heads of v that share them.  in: [B, n, H, K] float32.
+template <typename T>
+__global__ __launch_bounds__(256) void heinsen_attention_share(const float *in_q, const float *in_k, T *out_q, T *out_k, const int64_t *starts,
+                                                               int64_t n, int B, int Hk, int share, int K)
+{
+    const int64_t row = (int64_t)Hk * K, size = B * n * row, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += step) {
+        const int64_t token = i / row, b = token / n, head = i / K;
+        int64_t first;
+        if (token - b * n >= sequence(starts, n, (int)b, first)) continue;
+        const int c = (int)(i - head * K);
+        float q = 0.0f, k = 0.0f;
+        for (int j = 0; j < share; ++j) {
+            const int64_t at = (head * share + j) * K + c;
+            q += in_q[at], k += in_k[at];
+        }
+        const int64_t to = (first + token - b * n) * row + (i - token * row);
+        out_q[to] = (T)q;
+        out_k[to] = (T)k;
+    }
+}
+
+// Gradient of a decay for each head: the sum over all tokens.  in: [B, n, H] float32.
+template <typename T>
+__global__ __launch_bounds__(256) void heinsen_attention_decay_sum(const float *in, T *out, const int64_t *starts, int64_t n, int B, int H)
+{
+    __shared__ double part[256];
+    double sum = 0.0;
+    for (int b = 0; b < B; ++b) {
+        int64_t first;
+        const int64_t len = sequence(starts, n, b, first);
+        for (int64_t t = threadIdx.x; t < len; t += 256) sum += in[(b * n + t) * H + blockIdx.x];
+    }
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    for (int by = 128; by > 0; by /= 2) {
+        if (threadIdx.x < by) part[threadIdx.x] += part[threadIdx.x + by];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) out[blockIdx.x] = (T)(float)part[0];
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------
+
+bool rows16(const void *p, int64_t stride, int d, size_t size)
+{
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && d * size % 16 == 0;
+}
+
+template <typename T, int C, int DK, int DV> hipError_t backward_sized(const BackwardArgs &a, int64_t blocks, hipStream_t stream)
+{
+    heinsen_attention_backward<T, C, DK, DV><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int C> hipError_t backward(const BackwardArgs &a, int64_t blocks, hipStream_t stream)
+{
+    if (a.K <= 64) return a.V <= 64 ? backward_sized<T, C, 64, 64>(a, blocks, stream) : backward_sized<T, C, 64, 128>(a, blocks, stream);
+    return a.V <= 64 ? backward_sized<T, C, 128, 64>(a, blocks, stream) : backward_sized<T, C, 128, 128>(a, blocks, stream);
+}
+
+template <typename T> hipError_t step_backward(const BackwardArgs &a, const AttentionCall &c, int64_t blocks)
+{
+    bool whole = c.V % 4 == 0;
+    for (const void *p : {(const void *)c.s0, (const void *)c.grad_sn, (const void *)c.grad_s0}) whole = whole && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+    if (whole) heinsen_attention_step_backward<T, 4><<<dim3((unsigned)blocks), 256, 0, c.stream>>>(a, c.s0);
+    else heinsen_attention_step_backward<T, 1><<<dim3((unsigned)blocks), 256, 0, c.stream>>>(a, c.s0);
+    return hipGetLastError();
+}
+
+// Parts of the scratch, in this order.
+struct Parts {
+    Segments segments;
+    int chunks; // of the longest sequence
+    size_t states, gradients, chunk_states, shared, decays, all;
+};
+
+Parts parts(const AttentionCall &c)
+{
+    Parts s = {};
+    const bool few = c.n <= kFewTokens;
+    s.segments = few ? Segments{c.n, 1} : attention_segments(c);
+    const size_t size = c.bf16 ? 2 : 4, heads = (size_t)c.B * c.H, tokens = (size_t)c.B * c.n;
+    const int C = attention_chunk_tokens(c.bf16);
+    s.chunks = (int)((c.n + C - 1) / C);
+    s.states = s.gradients = segment_scratch(c, s.segments);
+    s.chunk_states = few ? 0 : align_up(heads * s.chunks * (c.K <= 64 ? 64 : 128) * (c.V <= 64 ? 64 : 128) * size, 256);
+    s.shared = c.share > 1 ? align_up(tokens * c.H * c.K * sizeof(float), 256) : 0;
+    s.decays = c.per_head && c.grad_log_a ? align_up(tokens * c.H * sizeof(float), 256) : 0;
+    s.all = s.states + s.gradients + s.chunk_states + 2 * s.shared + s.decays;
+    return s;
+}
+
+template <typename T> hipError_t finish(const AttentionCall &c, const float *shared_q, const float *shared_k, const float *decays)
+{
+    if (c.share > 1) {
+        heinsen_attention_share<T><<<4 * compute_units(), 256, 0, c.stream>>>(shared_q, shared_k, static_cast<T *>(c.grad_q), static_cast<T *>(c.grad_k),
+                                                                             c.starts, c.n, c.B, c.H / c.share, c.share, c.K);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (c.per_head && c.grad_log_a) {
+        heinsen_attention_decay_sum<T><<<c.H, 256, 0, c.stream>>>(decays, static_cast<T *>(c.grad_log_a), c.starts, c.n, c.B, c.H);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+} // namespace
+
+size_t attention_backward_scratch(const AttentionCall &c) { return parts(c).all; }
+
+hipError_t attention_backward_launch(const AttentionCall &c, void *scratch)
+{
+    const Parts s = parts(c);
+    const size_t size = c.bf16 ? 2 : 4;
+    char *at = static_cast<char *>(scratch);
+    float *const segment_state = reinterpret_cast<float *>(at);
+    float *const segment_grad = reinterpret_cast<float *>(at += s.states);
+    void *const states = at += s.gradients;
+    float *const shared_q = reinterpret_cast<float *>(at += s.chunk_states);
+    float *const shared_k = reinterpret_cast<float *>(at += s.shared);
+    float *const decays = reinterpret_cast<float *>(at += s.shared);
+
+    hipError_t e = hipSuccess;
+    const bool few = c.n <= kFewTokens;
+    if (s.segments.count > 1) {
+        e = attention_segment_states(c, s.segments, false, segment_state);
+        if (e == hipSuccess) e = attention_segment_states(c, s.segments, true, segment_grad);
+    }
+    if (e == hipSuccess && !few) e = attention_chunk_states(c, s.segments, segment_state, states, s.chunks);
+    if (e != hipSuccess) return e;
+
+    BackwardArgs a = {};
+    a.q = c.q, a.k = c.k, a.v = c.v, a.log_a = c.log_a, a.grad_out = c.grad_out, a.grad_sn = c.grad_sn, a.starts = c.starts;
+    a.states = states, a.segment_grad = segment_grad;
+    a.grad_q = c.share > 1 ? shared_q : c.grad_q, a.grad_k = c.share > 1 ? shared_k : c.grad_k, a.grad_v = c.grad_v;
+    a.grad_log_a = c.per_head && c.grad_log_a ? decays : c.grad_log_a;
+    a.grad_s0 = c.grad_s0;
+    a.n = c.n, a.q_stride = c.q_stride, a.k_stride = c.k_stride, a.v_stride = c.v_stride, a.segment = s.segments.tokens;
+    a.H = c.H, a.share = c.share, a.K = c.K, a.V = c.V, a.segments = s.segments.count, a.chunks = s.chunks;
+    a.scale = c.scale, a.per_head = c.per_head;
+    a.q_whole = rows16(c.q, c.q_stride, c.K, size), a.k_whole = rows16(c.k, c.k_stride, c.K, size), a.v_whole = rows16(c.v, c.v_stride, c.V, size);
+    a.out_whole = rows16(c.grad_out, (int64_t)c.H * c.V, c.V, size);
+    const size_t qk_size = c.share > 1 ? 4 : size;
+    a.grad_qk_whole = c.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.grad_q) % (4 * qk_size) == 0 && reinterpret_cast<uintptr_t>(a.grad_k) % (4 * qk_size) == 0;
+    a.grad_v_whole = c.V % 4 == 0 && reinterpret_cast<uintptr_t>(c.grad_v) % (4 * size) == 0;
+    const int64_t blocks = (int64_t)c.B * c.H * s.segments.count;
+    if (few) e = c.bf16 ? step_backward<__bf16>(a, c, blocks) : step_backward<float>(a, c, blocks);
+    else e = c.bf16 ? backward<__bf16, 64>(a, blocks, c.stream) : backward<float, 32>(a, blocks, c.stream);
+    if (e != hipSuccess) return e;
+    return c.bf16 ? finish<__bf16>(c, shared_q, shared_k, decays) : finish<float>(c, shared_q, shared_k, decays);
+}
+
+} // namespace hs
