@@ -26,8 +26,9 @@ struct SweepArgs {
     float *segment_state;    // [B, H, segments, K, V]: kSegment...: written; else, where there are several: the state at its start
     float *segment_decay;    // [B, H, segments]: written by kSegment...
     int H, share, K, V, segments, chunks;
+    int units, slices;       // heads and segments of all sequences; workgroups to each, DV columns of v apart
     float scale;
-    bool per_head, q_whole, k_whole, v_whole, out_whole;
+    bool per_head;
 };
 
 // The fragment with zeros in the place of infinite and NaN entries.
@@ -39,64 +40,81 @@ template <typename F> __device__ static inline F finite(F f)
     return f;
 }
 
-// A workgroup takes one segment of one head's tokens and goes through its chunks, the state in registers: each wave has a
-// slice of DV / 4 columns.  kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
+// Work of a workgroup: workgroup i runs on die i % 8, and the slices of a unit, which read the same q and k, go to one die.
+__device__ static inline int unit_and_slice(int slices, int &slice)
+{
+    slice = blockIdx.x / 8 % slices;
+    return blockIdx.x / (8 * slices) * 8 + blockIdx.x % 8;
+}
+
+// A workgroup takes one segment of one head's tokens and goes through its chunks, DV columns of the state in registers: each
+// wave has a quarter of them.  kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
 // (k, v) and gives the segment's own part of the gradient of the state it starts from.
 template <typename T, int C, int DK, int DV, int SWEEP>
 __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs p)
 {
-    constexpr int KT = DK / 16, NT = DV / 16 / kWaves, TT = C / 16, PK = pitch<T>(DK), PV = pitch<T>(DV), PP = pitch<T>(C);
+    constexpr int KT = DK / 16, NT = DV / 16 / kWaves, TT = C / 16;
     constexpr bool BACK = SWEEP == kSegmentGradient;
     // v scaled by its decay is summed into the state as the sum of this many bfloat16 numbers: three hold 24 bits
     constexpr int PLANES = sizeof(T) == 4 ? 1 : 3;
-    __shared__ __align__(16) T ks[C * PK];
-    __shared__ __align__(16) T vs[C * PV];
-    __shared__ __align__(16) T qs[SWEEP == kOutput ? C * PK : 16];
-    __shared__ __align__(16) T ps[SWEEP == kOutput ? C * PP : 16];
+    __shared__ __align__(16) T ks[C * DK];
+    __shared__ __align__(16) T vs[C * DV];
+    __shared__ __align__(16) T qs[SWEEP == kOutput ? C * DK : 16];
+    __shared__ __align__(16) T ps[SWEEP == kOutput ? C * C : 16];
     __shared__ Decays<C> decays;
     __shared__ int not_finite[2]; // of even and odd chunks
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int seg = blockIdx.x % p.segments, bh = blockIdx.x / p.segments, h = bh % p.H, b = bh / p.H;
+    const int lane0 = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane0 & 15, g = lane0 >> 4;
+    int slice;
+    const int unit = unit_and_slice(p.slices, slice);
+    if (unit >= p.units) return;
+    const int seg = unit % p.segments, bh = unit / p.segments, h = bh % p.H, b = bh / p.H;
     int64_t first;
     const int64_t len = sequence(p.starts, p.n, b, first);
     const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
     if (begin >= len && (seg > 0 || SWEEP != kOutput)) return;
 
+    const int v0 = slice * DV, V = p.V - v0 < DV ? p.V - v0 : DV; // of this workgroup's columns
     const T *const k = static_cast<const T *>(p.k) + first * p.k_stride + (int64_t)(h / p.share) * p.K;
     const T *const q = static_cast<const T *>(p.q) + first * p.q_stride + (int64_t)(h / p.share) * p.K;
-    const T *const v = static_cast<const T *>(p.v) + first * p.v_stride + (int64_t)h * p.V;
+    const T *const v = static_cast<const T *>(p.v) + first * p.v_stride + (int64_t)h * p.V + v0;
     const T *const log_a = static_cast<const T *>(p.log_a);
-    const int col = wave * (DV / kWaves) + r; // of this lane's first column
+    // the column of v that row or column r of this wave's block j stands for
+    auto column = [&](int j, int r) { return NT > 1 ? paired<T>(wave * NT + j, r) : 16 * wave + r; };
+    auto load_values = [&](const T *tile, int j, int k0, int lane) {
+        return NT > 1 ? load_paired<DV>(tile, wave * NT + j, k0, lane) : load_cols<DV>(tile, 16 * wave, k0, lane);
+    };
 
     f32x4 state[KT][NT];
     const bool segment_start = (SWEEP == kOutput || SWEEP == kChunkStates) && p.segments > 1 && begin < len;
-    const float *const from = segment_start ? p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V
-                              : (SWEEP == kOutput || SWEEP == kChunkStates) && p.s0 ? p.s0 + (int64_t)bh * p.K * p.V : nullptr;
+    const float *const from = segment_start ? p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0
+                              : (SWEEP == kOutput || SWEEP == kChunkStates) && p.s0 ? p.s0 + (int64_t)bh * p.K * p.V + v0 : nullptr;
 #pragma unroll
     for (int i = 0; i < KT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < NT; ++j) {
+            state[i][j] = f32x4{0, 0, 0, 0};
+            if (from)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = 16 * i + 4 * g + e, c = col + 16 * j;
-                state[i][j][e] = from && row < p.K && c < p.V ? from[(int64_t)row * p.V + c] : 0.0f;
-            }
+                for (int e = 0; e < 4; ++e) {
+                    const int row = paired<T>(i, 4 * g + e), c = column(j, r);
+                    const float x = from[(uint32_t)((row < p.K ? row : 0) * p.V + (c < V ? c : 0))];
+                    state[i][j][e] = row < p.K && c < V ? x : 0.0f;
+                }
+        }
     double total = 0.0; // log2 of the decay so far (wave 0)
 
     const int chunks = (int)((end - begin + C - 1) / C);
     auto chunk_start = [&](int i) { return begin + (int64_t)(BACK ? chunks - 1 - i : i) * C; };
     TileLoad<T, C, DK, kThreads> next_q, next_k;
     TileLoad<T, C, DV, kThreads> next_v;
-    float next_log_a = 0.0f;
+    T next_log_a = (T)0.0f;
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K, p.k_whole);
-        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, p.V, p.v_whole);
-        if (SWEEP == kOutput) next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K, p.q_whole);
-        if (wave == 0)
-            next_log_a = log_a == nullptr || lane >= rows ? 0.0f
-                         : p.per_head ? to_float(log_a[h]) : to_float(log_a[(first + t0 + lane) * p.H + h]);
+        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K);
+        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, V);
+        if (SWEEP == kOutput) next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K);
+        if (log_a) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
     };
     if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
     if (chunks > 0) request(chunk_start(0));
@@ -105,11 +123,16 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int64_t t0 = chunk_start(chunk);
         const int rows = (int)(end - t0 < C ? end - t0 : C);
+        next_k.settle(rows, p.K);
         next_k.store(ks);
+        next_v.settle(rows, V);
         next_v.store(vs);
-        if (SWEEP == kOutput) next_q.store(qs);
+        if (SWEEP == kOutput) {
+            next_q.settle(rows, p.K);
+            next_q.store(qs);
+        }
         if (next_v.not_finite()) atomicOr(&not_finite[chunk & 1], 1);
-        if (wave == 0) total += write_decays<C>(decays, next_log_a, lane);
+        if (wave == 0) total += write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
         __syncthreads();
         const bool odd_values = not_finite[chunk & 1] != 0;
         if (threadIdx.x == 0) not_finite[(chunk + 1) & 1] = 0;
@@ -119,43 +142,50 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
             // the weights of the chunk's tokens for one another, scale e^{G_t-G_s} q_t . k_s, in tiles of 16 x 16: this wave's
             // are those of tokens t in one row of tiles
             const int tt = wave % TT;
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
             Frag<T> qf[DK / 32];
 #pragma unroll
-            for (int i = 0; i < DK / 32; ++i) qf[i] = load_rows(qs, PK, 16 * tt, 32 * i, lane);
+            for (int i = 0; i < DK / 32; ++i) qf[i] = load_rows<DK>(qs, 16 * tt, 32 * i, lane);
             const float whole_t = decays.whole[16 * tt + r], part_t = decays.part[16 * tt + r];
             for (int st = wave / TT; st <= (tt | 1); st += kWaves / TT) {
                 f32x4 acc = {0, 0, 0, 0};
                 if (st <= tt) {
 #pragma unroll
-                    for (int i = 0; i < DK / 32; ++i) acc = mma(load_rows(ks, PK, 16 * st, 32 * i, lane), qf[i], acc);
+                    for (int i = 0; i < DK / 32; ++i) acc = mma(load_rows<DK>(ks, 16 * st, 32 * i, lane), qf[i], acc);
+                    const f32x4 whole = *reinterpret_cast<const f32x4 *>(&decays.whole[16 * st + 4 * g]);
+                    const f32x4 part = *reinterpret_cast<const f32x4 *>(&decays.part[16 * st + 4 * g]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int s = 16 * st + 4 * g + e;
-                        const float w = __builtin_amdgcn_exp2f((whole_t - decays.whole[s]) + (part_t - decays.part[s])) * p.scale;
-                        acc[e] = s <= 16 * tt + r ? acc[e] * w : 0.0f;
+                        const float w = __builtin_amdgcn_exp2f((whole_t - whole[e]) + (part_t - part[e])) * p.scale;
+                        acc[e] = 16 * st + 4 * g + e <= 16 * tt + r ? acc[e] * w : 0.0f;
                     }
                 }
-                *reinterpret_cast<x4<T> *>(ps + (16 * tt + r) * PP + 16 * st + 4 * g) = __builtin_convertvector(acc, x4<T>);
+                *reinterpret_cast<x4<T> *>(ps + at<T, C>(16 * tt + r, 16 * st + 4 * g)) = __builtin_convertvector(acc, x4<T>);
             }
             __syncthreads();
         }
         if (SWEEP == kChunkStates) {
-            T *const to = static_cast<T *>(p.out) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV);
+            T *const to = static_cast<T *>(p.out) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV * p.slices) + v0 * DK;
 #pragma unroll
             for (int i = 0; i < KT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) to[(16 * i + 4 * g + e) * DV + col + 16 * j] = (T)state[i][j][e];
+                    *reinterpret_cast<x4<T> *>(to + column(j, r) * DK + paired<T>(i, 4 * g)) = __builtin_convertvector(state[i][j], x4<T>);
         }
 
         Frag<T> vf[C / 32][NT];
 #pragma unroll
         for (int i = 0; i < C / 32; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) vf[i][j] = load_cols(vs, PV, wave * (DV / kWaves) + 16 * j, 32 * i, lane);
+            for (int j = 0; j < NT; ++j) vf[i][j] = load_values(vs, j, 32 * i, fresh(lane0));
 
         if (SWEEP == kOutput) {
+            if (odd_values)
+#pragma unroll
+                for (int i = 0; i < C / 32; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) vf[i][j] = finite(vf[i][j]);
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
             f32x4 o[TT][NT]; // rows: columns of v, columns: tokens
 #pragma unroll
             for (int i = 0; i < TT; ++i)
@@ -168,7 +198,7 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
                 for (int j = 0; j < NT; ++j) sf[j] = to_frag<T>(state[2 * i][j], state[2 * i + 1][j]);
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
-                    const Frag<T> qf = load_rows(qs, PK, 16 * t, 32 * i, lane);
+                    const Frag<T> qf = load_rows<DK>(qs, 16 * t, 32 * i, lane);
 #pragma unroll
                     for (int j = 0; j < NT; ++j) o[t][j] = mma(sf[j], qf, o[t][j]);
                 }
@@ -180,29 +210,35 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
                 for (int j = 0; j < NT; ++j) o[t][j] *= w;
 #pragma unroll
                 for (int i = 0; i <= t / 2; ++i) {
-                    const Frag<T> pf = load_rows(ps, PP, 16 * t, 32 * i, lane);
+                    const Frag<T> pf = load_rows<C>(ps, 16 * t, 32 * i, lane);
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) o[t][j] = mma(odd_values ? finite(vf[i][j]) : vf[i][j], pf, o[t][j]);
+                    for (int j = 0; j < NT; ++j) o[t][j] = mma(vf[i][j], pf, o[t][j]);
                 }
                 // an infinite or NaN v_s has no part in the tokens before it, where its zero weight would make it NaN: such
                 // values were left out above and are added to the tokens that see them
                 if (odd_values)
                     for (int s = 0; s <= 16 * t + r; ++s) {
-                        const float w = to_float(ps[(16 * t + r) * PP + s]);
+                        const float w = to_float(ps[at<T, C>(16 * t + r, s)]);
 #pragma unroll
                         for (int j = 0; j < NT; ++j)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float x = to_float(vs[s * PV + wave * (DV / kWaves) + 16 * j + 4 * g + e]);
+                                const float x = to_float(vs[at<T, DV>(s, column(j, 4 * g + e))]);
                                 if (!(__builtin_fabsf(x) < __builtin_inff())) o[t][j][e] += w * x;
                             }
                     }
                 if (16 * t + r < rows) {
-                    T *const row = static_cast<T *>(p.out) + ((first + t0 + 16 * t + r) * p.H + h) * (int64_t)p.V;
+                    T *const row = static_cast<T *>(p.out) + ((first + t0 + 16 * t + r) * p.H + h) * (int64_t)p.V + v0;
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) store4(row, wave * (DV / kWaves) + 16 * j + 4 * g, p.V, p.out_whole, o[t][j]);
+                    for (int j = 0; j < NT; ++j) store4(row, column(j, 4 * g), V, o[t][j]);
                 }
+                __builtin_amdgcn_sched_barrier(0); // loads of what follows would only take registers here
             }
+            if (odd_values)
+#pragma unroll
+                for (int i = 0; i < C / 32; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) vf[i][j] = load_values(vs, j, 32 * i, fresh(lane0));
         }
 
         // the state after the chunk
@@ -213,13 +249,14 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
             for (int j = 0; j < NT; ++j) state[i][j] *= decay;
 #pragma unroll
         for (int i = 0; i < C / 32; ++i) {
-            const float *const w = (BACK ? decays.from_start : decays.to_end) + 32 * i + 4 * g;
+            const int lane = fresh(lane0), g = lane >> 4;
+            const float *const w = (BACK ? decays.from_start : decays.to_end) + 32 * i;
             Frag<T> vw[NT][PLANES];
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float x = to_float(vf[i][j][e]) * w[(e >> 2) * 16 + (e & 3)];
+                    float x = to_float(vf[i][j][e]) * w[step_of<T>(g, e)];
                     if (BACK) x *= p.scale;
 #pragma unroll
                     for (int plane = 0; plane < PLANES; ++plane) {
@@ -231,7 +268,7 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
                 }
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                const Frag<T> kf = load_cols(ks, PK, 16 * kt, 32 * i, lane);
+                const Frag<T> kf = load_paired<DK>(ks, kt, 32 * i, lane);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -246,16 +283,16 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (16 * i + 4 * g + e >= p.K) state[i][j][e] = 0.0f;
+                        if (paired<T>(i, 4 * g + e) >= p.K) state[i][j][e] = 0.0f;
         __syncthreads();
     }
 
     float *to = nullptr;
     if (SWEEP == kSegmentState || SWEEP == kSegmentGradient) {
-        to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V;
-        if (threadIdx.x == 0) p.segment_decay[(int64_t)bh * p.segments + seg] = __builtin_amdgcn_exp2f((float)total);
+        to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0;
+        if (threadIdx.x == 0 && slice == 0) p.segment_decay[(int64_t)bh * p.segments + seg] = __builtin_amdgcn_exp2f((float)total);
     } else if (SWEEP == kOutput && p.sn && end == len) {
-        to = p.sn + (int64_t)bh * p.K * p.V;
+        to = p.sn + (int64_t)bh * p.K * p.V + v0;
     }
     if (to)
 #pragma unroll
@@ -264,8 +301,8 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int row = 16 * i + 4 * g + e, c = col + 16 * j;
-                    if (row < p.K && c < p.V) to[(int64_t)row * p.V + c] = state[i][j][e];
+                    const int row = paired<T>(i, 4 * g + e), c = column(j, r);
+                    if (row < p.K && c < V) to[(uint32_t)(row * p.V + c)] = state[i][j][e];
                 }
 }
 
@@ -292,7 +329,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_chain(float *segment_st
 // ---- few tokens -----------------------------------------------------------------------------------------------
 //
 // The recurrence itself, a token at a time: the state is read once, stays in registers and is written once, which is all
-// the memory traffic there is.  A workgroup has COLS columns of a head's state; a thread has VEC neighbouring columns of
+// the memory traffic there is.  A workgroup has COLS columns of a head's state; a thread has four neighbouring columns of
 // every ROWS-th row.
 struct StepArgs {
     const void *q, *k, *v, *log_a;
@@ -306,27 +343,24 @@ struct StepArgs {
     bool per_head;
 };
 
-template <typename T, int COLS, int VEC>
+template <typename T, int COLS>
 __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 {
-    constexpr int ACROSS = COLS / VEC, ROWS = 256 / ACROSS, PER = (128 + ROWS - 1) / ROWS, IN_WAVE = 64 / ACROSS > 1 ? 64 / ACROSS : 1;
-    constexpr int PARTS = ROWS / IN_WAVE; // partial sums of an output
-    typedef float vec __attribute__((ext_vector_type(VEC)));
+    constexpr int ACROSS = COLS / 4, ROWS = 256 / ACROSS, PER = 128 / ROWS;
     __shared__ float qk[2][128];
-    __shared__ float sums[PARTS][COLS];
+    __shared__ float sums[4][COLS];
     const int slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
-    const int row0 = threadIdx.x / ACROSS, local = threadIdx.x % ACROSS * VEC, col = slice * COLS + local;
-    const bool inside = col < p.V;
+    const int row0 = threadIdx.x / ACROSS, local = threadIdx.x % ACROSS * 4, col = slice * COLS + local;
     int64_t first;
     const int64_t len = sequence(p.starts, p.n, b, first);
-    const int64_t at = (int64_t)bh * p.K * p.V + col;
+    const int64_t at = (int64_t)bh * p.K * p.V;
 
-    vec state[PER];
+    f32x4 state[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int row = row0 + i * ROWS;
-        state[i] = (vec)0.0f;
-        if (p.s0 && inside && row < p.K) state[i] = *reinterpret_cast<const vec *>(p.s0 + at + (int64_t)row * p.V);
+        state[i] = f32x4{0, 0, 0, 0};
+        if (p.s0 && row < p.K) state[i] = load4(p.s0 + at + row * p.V, col, p.V);
     }
     for (int64_t t = 0; t < len; ++t) {
         const int64_t token = first + t;
@@ -339,14 +373,12 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
         const T *const log_a = static_cast<const T *>(p.log_a);
         const float la = log_a == nullptr ? 0.0f : to_float(log_a[p.per_head ? h : token * p.H + h]);
         const float a = la <= -104.0f ? 0.0f : expf(la);
-        vec value = (vec)0.0f;
-        if (inside) {
-            const T *const v = static_cast<const T *>(p.v) + token * p.v_stride + (int64_t)h * p.V + col;
+        const T *const v = static_cast<const T *>(p.v) + token * p.v_stride + (int64_t)h * p.V;
+        f32x4 value;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) value[e] = to_float(v[e]);
-        }
+        for (int e = 0; e < 4; ++e) value[e] = col + e < p.V ? to_float(v[col + e]) : 0.0f;
         __syncthreads();
-        vec o = (vec)0.0f;
+        f32x4 o = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int row = row0 + i * ROWS;
@@ -358,25 +390,21 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 #pragma unroll
         for (int by = ACROSS; by < 64; by *= 2)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) o[e] += __shfl_xor(o[e], by);
-        if (threadIdx.x % 64 < ACROSS || ACROSS > 64) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sums[row0 / IN_WAVE][local + e] = o[e];
-        }
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], by);
+        if (threadIdx.x % 64 < ACROSS) *reinterpret_cast<f32x4 *>(&sums[threadIdx.x / 64][local]) = o;
         __syncthreads();
         if (threadIdx.x < COLS && slice * COLS + threadIdx.x < p.V) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < PARTS; ++i) sum += sums[i][threadIdx.x];
-            static_cast<T *>(p.out)[(token * p.H + h) * p.V + slice * COLS + threadIdx.x] = (T)sum;
+            const int c = threadIdx.x;
+            const float sum = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+            static_cast<T *>(p.out)[(token * p.H + h) * p.V + slice * COLS + c] = (T)sum;
         }
         __syncthreads();
     }
-    if (p.sn && inside)
+    if (p.sn)
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int row = row0 + i * ROWS;
-            if (row < p.K) *reinterpret_cast<vec *>(p.sn + at + (int64_t)row * p.V) = state[i];
+            if (row < p.K) store4(p.sn + at + row * p.V, col, p.V, state[i]);
         }
 }
 
@@ -384,32 +412,27 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 
 template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 : 32; }
 
-bool rows16(const void *p, int64_t stride, int d, size_t size)
+template <typename T, int SWEEP, int DK, int DV> hipError_t sweep_sized(SweepArgs &a, hipStream_t stream)
 {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && d * size % 16 == 0;
-}
-
-template <typename T, int SWEEP, int DK, int DV> hipError_t sweep_sized(const SweepArgs &a, int64_t blocks, hipStream_t stream)
-{
+    a.slices = (a.V + DV - 1) / DV;
+    const int64_t blocks = ((int64_t)a.units + 7) / 8 * 8 * a.slices;
     heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int SWEEP> hipError_t sweep(const SweepArgs &a, int64_t blocks, hipStream_t stream)
+template <typename T, int SWEEP> hipError_t sweep(SweepArgs &a, hipStream_t stream)
 {
-    if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64>(a, blocks, stream) : sweep_sized<T, SWEEP, 64, 128>(a, blocks, stream);
-    return a.V <= 64 ? sweep_sized<T, SWEEP, 128, 64>(a, blocks, stream) : sweep_sized<T, SWEEP, 128, 128>(a, blocks, stream);
+    if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64>(a, stream) : sweep_sized<T, SWEEP, 64, 128>(a, stream);
+    return a.V <= 64 ? sweep_sized<T, SWEEP, 128, 64>(a, stream) : sweep_sized<T, SWEEP, 128, 128>(a, stream);
 }
 
-SweepArgs sweep_args(const AttentionCall &c)
+SweepArgs sweep_args(const AttentionCall &c, const Segments &s)
 {
-    const size_t size = c.bf16 ? 2 : 4;
     SweepArgs a = {};
     a.q = c.q, a.k = c.k, a.v = c.v, a.log_a = c.log_a, a.s0 = c.s0, a.starts = c.starts, a.out = c.out, a.sn = c.sn;
     a.n = c.n, a.q_stride = c.q_stride, a.k_stride = c.k_stride, a.v_stride = c.v_stride;
     a.H = c.H, a.share = c.share, a.K = c.K, a.V = c.V, a.scale = c.scale, a.per_head = c.per_head;
-    a.q_whole = rows16(c.q, c.q_stride, c.K, size), a.k_whole = rows16(c.k, c.k_stride, c.K, size), a.v_whole = rows16(c.v, c.v_stride, c.V, size);
-    a.out_whole = reinterpret_cast<uintptr_t>(c.out) % (4 * size) == 0 && c.V % 4 == 0;
+    a.segment = s.tokens, a.segments = s.count, a.units = c.B * c.H * s.count;
     return a;
 }
 
@@ -422,10 +445,10 @@ hipError_t chain(bool back, float *state, const float *decay, const float *init,
     return hipGetLastError();
 }
 
-template <typename T, int COLS, int VEC> hipError_t step_sized(StepArgs &a, const AttentionCall &c)
+template <typename T, int COLS> hipError_t step_sized(StepArgs &a, const AttentionCall &c)
 {
     a.slices = (c.V + COLS - 1) / COLS;
-    heinsen_attention_step<T, COLS, VEC><<<dim3((unsigned)((int64_t)c.B * c.H * a.slices)), 256, 0, c.stream>>>(a);
+    heinsen_attention_step<T, COLS><<<dim3((unsigned)((int64_t)c.B * c.H * a.slices)), 256, 0, c.stream>>>(a);
     return hipGetLastError();
 }
 
@@ -435,11 +458,9 @@ template <typename T> hipError_t step(const AttentionCall &c)
     a.q = c.q, a.k = c.k, a.v = c.v, a.log_a = c.log_a, a.s0 = c.s0, a.starts = c.starts, a.out = c.out, a.sn = c.sn;
     a.n = c.n, a.q_stride = c.q_stride, a.k_stride = c.k_stride, a.v_stride = c.v_stride;
     a.H = c.H, a.share = c.share, a.K = c.K, a.V = c.V, a.scale = c.scale, a.per_head = c.per_head;
-    const bool whole = c.V % 4 == 0 && reinterpret_cast<uintptr_t>(c.s0) % 16 == 0 && reinterpret_cast<uintptr_t>(c.sn) % 16 == 0;
-    if (!whole) return step_sized<T, 64, 1>(a, c);
     // narrow slices where heads alone do not fill the chip
-    if ((int64_t)c.B * c.H * 2 <= compute_units() && c.V > 32) return step_sized<T, 32, 4>(a, c);
-    return step_sized<T, 128, 4>(a, c);
+    if ((int64_t)c.B * c.H * 2 <= compute_units() && c.V > 32) return step_sized<T, 32>(a, c);
+    return step_sized<T, 128>(a, c);
 }
 
 } // namespace
@@ -467,19 +488,16 @@ size_t segment_scratch(const AttentionCall &c, const Segments &s)
 // The states at the segments' starts (BACK: the gradients at their ends) from the segments' own sums.
 hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, bool back, void *scratch)
 {
-    SweepArgs a = sweep_args(c);
-    a.segment = s.tokens, a.segments = s.count;
+    SweepArgs a = sweep_args(c, s);
     a.segment_state = static_cast<float *>(scratch);
     a.segment_decay = a.segment_state + align_up((size_t)c.B * c.H * s.count * c.K * c.V * sizeof(float), 256) / sizeof(float);
-    const int64_t blocks = (int64_t)c.B * c.H * s.count;
     hipError_t e;
     if (back) {
-        const size_t size = c.bf16 ? 2 : 4;
-        a.k = c.q, a.k_stride = c.q_stride, a.k_whole = a.q_whole;
-        a.v = c.grad_out, a.v_stride = (int64_t)c.H * c.V, a.v_whole = rows16(c.grad_out, a.v_stride, c.V, size);
-        e = c.bf16 ? sweep<__bf16, kSegmentGradient>(a, blocks, c.stream) : sweep<float, kSegmentGradient>(a, blocks, c.stream);
+        a.k = c.q, a.k_stride = c.q_stride;
+        a.v = c.grad_out, a.v_stride = (int64_t)c.H * c.V;
+        e = c.bf16 ? sweep<__bf16, kSegmentGradient>(a, c.stream) : sweep<float, kSegmentGradient>(a, c.stream);
     } else {
-        e = c.bf16 ? sweep<__bf16, kSegmentState>(a, blocks, c.stream) : sweep<float, kSegmentState>(a, blocks, c.stream);
+        e = c.bf16 ? sweep<__bf16, kSegmentState>(a, c.stream) : sweep<float, kSegmentState>(a, c.stream);
     }
     if (e != hipSuccess) return e;
     return chain(back, a.segment_state, a.segment_decay, back ? c.grad_sn : c.s0, c, s);
@@ -487,11 +505,10 @@ hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, b
 
 hipError_t attention_chunk_states(const AttentionCall &c, const Segments &s, float *segment_state, void *states, int chunks)
 {
-    SweepArgs a = sweep_args(c);
-    a.segment = s.tokens, a.segments = s.count, a.segment_state = segment_state;
+    SweepArgs a = sweep_args(c, s);
+    a.segment_state = segment_state;
     a.out = states, a.chunks = chunks;
-    const int64_t blocks = (int64_t)c.B * c.H * s.count;
-    return c.bf16 ? sweep<__bf16, kChunkStates>(a, blocks, c.stream) : sweep<float, kChunkStates>(a, blocks, c.stream);
+    return c.bf16 ? sweep<__bf16, kChunkStates>(a, c.stream) : sweep<float, kChunkStates>(a, c.stream);
 }
 
 int attention_chunk_tokens(bool bf16) { return bf16 ? chunk_tokens<__bf16>() : chunk_tokens<float>(); }
@@ -506,10 +523,9 @@ hipError_t attention_launch(const AttentionCall &c, void *scratch)
         const hipError_t e = attention_segment_states(c, s, false, scratch);
         if (e != hipSuccess) return e;
     }
-    SweepArgs a = sweep_args(c);
-    a.segment = s.tokens, a.segments = s.count, a.segment_state = static_cast<float *>(scratch);
-    const int64_t blocks = (int64_t)c.B * c.H * s.count;
-    return c.bf16 ? sweep<__bf16, kOutput>(a, blocks, c.stream) : sweep<float, kOutput>(a, blocks, c.stream);
+    SweepArgs a = sweep_args(c, s);
+    a.segment_state = static_cast<float *>(scratch);
+    return c.bf16 ? sweep<__bf16, kOutput>(a, c.stream) : sweep<float, kOutput>(a, c.stream);
 }
 
 } // namespace hs

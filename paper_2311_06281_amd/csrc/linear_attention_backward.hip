@@ -22,7 +22,7 @@ struct BackwardArgs {
     const void *q, *k, *v, *log_a, *grad_out;
     const float *grad_sn;
     const int64_t *starts;
-    const void *states;           // [B, H, chunks, DK, DV] in T: the state at each chunk's start
+    const void *states;           // [B, H, chunks, DV, DK] in T: the state at each chunk's start, transposed
     const float *segment_grad;    // [B, H, segments, K, V]: where there are several, the gradient of the state at each one's end
     void *grad_q, *grad_k;        // T, or float for each head of v where heads share q and k
     void *grad_v, *grad_log_a;    // grad_log_a: T, or float [tokens, H] with per_head, or null
@@ -30,7 +30,7 @@ struct BackwardArgs {
     int64_t n, q_stride, k_stride, v_stride, segment;
     int H, share, K, V, segments, chunks;
     float scale;
-    bool per_head, q_whole, k_whole, v_whole, out_whole, grad_qk_whole, grad_v_whole;
+    bool per_head;
 };
 
 // A workgroup takes one segment of one head's tokens from its last chunk to its first; the gradient R of the state is in
@@ -39,19 +39,20 @@ template <typename T, int C, int DK, int DV>
 __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(BackwardArgs p)
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
-    constexpr int PK = pitch<T>(DK), PV = pitch<T>(DV), PP = pitch<T>(C);
     constexpr int PLANES = sizeof(T) == 4 ? 1 : 3; // of q do^T's operand, see heinsen_attention_sweep
-    __shared__ __align__(16) T qs[C * PK];
-    __shared__ __align__(16) T ks[C * PK];
-    __shared__ __align__(16) T vs[C * PV];
-    __shared__ __align__(16) T os[C * PV];  // grad_out
-    __shared__ __align__(16) T rs[DV * PK]; // R transposed
-    __shared__ __align__(16) T ps[C * PP];  // P transposed: [s][t]
-    __shared__ __align__(16) T ds[C * PP];  // D transposed
+    constexpr bool STAGED = sizeof(T) == 2;        // the chunk's first state goes through LDS; in float32 there is no room
+    __shared__ __align__(16) T qs[C * DK];
+    __shared__ __align__(16) T ks[C * DK];
+    __shared__ __align__(16) T vs[C * DV];
+    __shared__ __align__(16) T os[C * DV];  // grad_out
+    __shared__ __align__(16) T rs[DV * DK]; // R transposed
+    __shared__ __align__(16) T ss[STAGED ? DV * DK : 16]; // S transposed
+    __shared__ __align__(16) T ps[C * C];   // P transposed: [s][t]
+    __shared__ __align__(16) T ds[C * C];   // D transposed
     __shared__ Decays<C> decays;
     __shared__ float xs[KT][C], ys[KT][C], pair_rows[TT][C], pair_cols[TT][C], spans[WAVES];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    const int lane0 = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane0 & 15, g = lane0 >> 4;
     const int seg = blockIdx.x % p.segments, bh = blockIdx.x / p.segments, h = bh % p.H, b = bh / p.H;
     int64_t first;
     const int64_t len = sequence(p.starts, p.n, b, first);
@@ -73,51 +74,63 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int row = 16 * i + 4 * g + e;
-            grad[i][e] = from && row < p.K && col < p.V ? from[(int64_t)row * p.V + col] : 0.0f;
+            const int row = paired<T>(i, 4 * g + e);
+            grad[i][e] = 0.0f;
+            if (from) {
+                const float x = from[(uint32_t)((row < p.K ? row : 0) * p.V + (col < p.V ? col : 0))];
+                grad[i][e] = row < p.K && col < p.V ? x : 0.0f;
+            }
         }
 
     const int chunks = (int)((end - begin + C - 1) / C);
     TileLoad<T, C, DK, THREADS> next_q, next_k;
     TileLoad<T, C, DV, THREADS> next_v, next_o;
-    float next_log_a = 0.0f;
+    TileLoad<T, STAGED ? DV : THREADS * 16 / (int)sizeof(T) / DK, DK, THREADS> next_s;
+    T next_log_a = (T)0.0f;
+    auto state_of = [&](int64_t t0) { return static_cast<const T *>(p.states) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV); };
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K, p.q_whole);
-        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K, p.k_whole);
-        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, p.V, p.v_whole);
-        next_o.load(o + t0 * o_stride, o_stride, rows, p.V, p.out_whole);
-        if (wave == 0)
-            next_log_a = log_a == nullptr || lane >= rows ? 0.0f
-                         : p.per_head ? to_float(log_a[h]) : to_float(log_a[(first + t0 + lane) * p.H + h]);
+        next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K);
+        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K);
+        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, p.V);
+        next_o.load(o + t0 * o_stride, o_stride, rows, p.V);
+        if (STAGED) next_s.load(state_of(t0), DK, DV, DK);
+        if (log_a) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
     };
     if (chunks > 0) request(begin + (int64_t)(chunks - 1) * C);
 
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
         const int64_t t0 = begin + (int64_t)chunk * C;
         const int rows = (int)(end - t0 < C ? end - t0 : C);
+        next_q.settle(rows, p.K);
         next_q.store(qs);
+        next_k.settle(rows, p.K);
         next_k.store(ks);
+        next_v.settle(rows, p.V);
         next_v.store(vs);
+        next_o.settle(rows, p.V);
         next_o.store(os);
-        if (wave == 0) write_decays<C>(decays, next_log_a, lane);
+        if (STAGED) next_s.store(ss);
+        if (wave == 0) write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
 #pragma unroll
-        for (int i = 0; i < KT; ++i) *reinterpret_cast<x4<T> *>(rs + col * PK + 16 * i + 4 * g) = __builtin_convertvector(grad[i], x4<T>);
+        for (int i = 0; i < KT; ++i)
+            *reinterpret_cast<x4<T> *>(rs + at<T, DK>(col, paired<T>(i, 4 * g))) = __builtin_convertvector(grad[i], x4<T>);
         __syncthreads();
         if (chunk > 0) request(t0 - C);
-        const T *const state = static_cast<const T *>(p.states) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV);
+        const T *const state = state_of(t0);
 
         // P, D and the pairs' sums, in tiles of 16 x 16 on and below the diagonal, and zeros beside it where a product
         // takes two tiles at a time
-        for (int at = wave; at < TT * TT; at += WAVES) {
-            const int tt = at / TT, st = at % TT;
+        for (int tile = wave; tile < TT * TT; tile += WAVES) {
+            const int tt = tile / TT, st = tile % TT;
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
             if (st > (tt | 1)) continue;
             f32x4 pt = {0, 0, 0, 0}, dt = {0, 0, 0, 0};
             if (st <= tt) {
 #pragma unroll
-                for (int i = 0; i < DK / 32; ++i) pt = mma(load_rows(qs, PK, 16 * tt, 32 * i, lane), load_rows(ks, PK, 16 * st, 32 * i, lane), pt);
+                for (int i = 0; i < DK / 32; ++i) pt = mma(load_rows<DK>(qs, 16 * tt, 32 * i, lane), load_rows<DK>(ks, 16 * st, 32 * i, lane), pt);
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) dt = mma(load_rows(os, PV, 16 * tt, 32 * i, lane), load_rows(vs, PV, 16 * st, 32 * i, lane), dt);
+                for (int i = 0; i < DV / 32; ++i) dt = mma(load_rows<DV>(os, 16 * tt, 32 * i, lane), load_rows<DV>(vs, 16 * st, 32 * i, lane), dt);
                 const int s = 16 * st + r; // rows: tokens t, columns: tokens s
                 const float whole_s = decays.whole[s], part_s = decays.part[s];
                 float below = 0.0f;
@@ -141,13 +154,14 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                     for (int e = 0; e < 4; ++e) across[e] += __shfl_xor(across[e], by);
                 if (r == 0) *reinterpret_cast<f32x4 *>(&pair_rows[st][16 * tt + 4 * g]) = across;
             }
-            *reinterpret_cast<x4<T> *>(ps + (16 * st + r) * PP + 16 * tt + 4 * g) = __builtin_convertvector(pt, x4<T>);
-            *reinterpret_cast<x4<T> *>(ds + (16 * st + r) * PP + 16 * tt + 4 * g) = __builtin_convertvector(dt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ps + at<T, C>(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(pt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ds + at<T, C>(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(dt, x4<T>);
         }
         __syncthreads();
 
         // dv, rows: this wave's columns of v, columns: tokens s
         {
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
             Frag<T> rf[DK / 32];
 #pragma unroll
             for (int i = 0; i < DK / 32; ++i) rf[i] = to_frag<T>(grad[2 * i], grad[2 * i + 1]);
@@ -155,34 +169,38 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             for (int st = 0; st < TT; ++st) {
                 f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < DK / 32; ++i) acc = mma(rf[i], load_rows(ks, PK, 16 * st, 32 * i, lane), acc);
+                for (int i = 0; i < DK / 32; ++i) acc = mma(rf[i], load_rows<DK>(ks, 16 * st, 32 * i, lane), acc);
                 acc *= decays.to_end[16 * st + r];
 #pragma unroll
                 for (int i = st / 2; i < C / 32; ++i)
-                    acc = mma(load_cols(os, PV, 16 * wave, 32 * i, lane), load_rows(ps, PP, 16 * st, 32 * i, lane), acc);
+                    acc = mma(load_cols<DV>(os, 16 * wave, 32 * i, lane), load_rows<C>(ps, 16 * st, 32 * i, lane), acc);
                 if (16 * st + r < rows)
-                    store4(static_cast<T *>(p.grad_v) + ((first + t0 + 16 * st + r) * p.H + h) * (int64_t)p.V, 16 * wave + 4 * g, p.V,
-                           p.grad_v_whole, acc);
+                    store4(static_cast<T *>(p.grad_v) + ((first + t0 + 16 * st + r) * p.H + h) * (int64_t)p.V, 16 * wave + 4 * g, p.V, acc);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         // dq and dk: 16 columns of q and k at a time, tokens in the columns
         for (int kt = wave % KT; kt < KT; kt += WAVES) {
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
             Frag<T> sf[DV / 32], rf[DV / 32];
 #pragma unroll
             for (int i = 0; i < DV / 32; ++i) {
-                const T *const at = state + (16 * kt + r) * DV + 32 * i + 4 * g;
-                sf[i] = join<T>(*reinterpret_cast<const x4<T> *>(at), *reinterpret_cast<const x4<T> *>(at + 16));
-                rf[i] = load_cols(rs, PK, 16 * kt, 32 * i, lane);
+                if (STAGED) sf[i] = load_cols<DK>(ss, 16 * kt, 32 * i, lane);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sf[i][e] = state[(32 * i + step_of<T>(g, e)) * DK + 16 * kt + r];
+                rf[i] = load_cols<DK>(rs, 16 * kt, 32 * i, lane);
             }
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
+                const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
                 if (WAVES > KT && (t % (WAVES / KT > 0 ? WAVES / KT : 1)) != wave / KT) continue;
                 const int token = 16 * t + r;
                 f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) acc = mma(sf[i], load_rows(os, PV, 16 * t, 32 * i, lane), acc);
+                for (int i = 0; i < DV / 32; ++i) acc = mma(sf[i], load_rows<DV>(os, 16 * t, 32 * i, lane), acc);
                 acc *= decays.from_start[token] * p.scale;
-                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + token * PK + 16 * kt + 4 * g);
+                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + at<T, DK>(token, 16 * kt + 4 * g));
                 float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
@@ -191,19 +209,19 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 if (g == 0) xs[kt][token] = sum;
 #pragma unroll
                 for (int i = 0; i <= t / 2; ++i)
-                    acc = mma(load_cols(ks, PK, 16 * kt, 32 * i, lane), load_cols(ds, PP, 16 * t, 32 * i, lane), acc);
+                    acc = mma(load_cols<DK>(ks, 16 * kt, 32 * i, lane), load_cols<C>(ds, 16 * t, 32 * i, lane), acc);
                 // a head of v's own part of a shared gradient goes to the scratch, n places for each sequence
                 const int64_t place = (p.share > 1 ? b * p.n : first) + t0 + token;
                 if (token < rows) {
-                    if (p.share > 1) store4(static_cast<float *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
-                    else store4(static_cast<T *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
+                    if (p.share > 1) store4(static_cast<float *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
+                    else store4(static_cast<T *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
                 }
 
                 acc = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) acc = mma(rf[i], load_rows(vs, PV, 16 * t, 32 * i, lane), acc);
+                for (int i = 0; i < DV / 32; ++i) acc = mma(rf[i], load_rows<DV>(vs, 16 * t, 32 * i, lane), acc);
                 acc *= decays.to_end[token];
-                own = *reinterpret_cast<const x4<T> *>(ks + token * PK + 16 * kt + 4 * g);
+                own = *reinterpret_cast<const x4<T> *>(ks + at<T, DK>(token, 16 * kt + 4 * g));
                 sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
@@ -212,11 +230,12 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 if (g == 0) ys[kt][token] = sum;
 #pragma unroll
                 for (int i = t / 2; i < C / 32; ++i)
-                    acc = mma(load_cols(qs, PK, 16 * kt, 32 * i, lane), load_rows(ds, PP, 16 * t, 32 * i, lane), acc);
+                    acc = mma(load_cols<DK>(qs, 16 * kt, 32 * i, lane), load_rows<C>(ds, 16 * t, 32 * i, lane), acc);
                 if (token < rows) {
-                    if (p.share > 1) store4(static_cast<float *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
-                    else store4(static_cast<T *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, p.grad_qk_whole, acc);
+                    if (p.share > 1) store4(static_cast<float *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
+                    else store4(static_cast<T *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
                 }
+                __builtin_amdgcn_sched_barrier(0); // loads of the next tokens would only take registers here
             }
         }
         // <R, S>, and R at the chunk's start
@@ -225,20 +244,23 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < KT; ++i) {
+                const x4<T> s = STAGED ? *reinterpret_cast<const x4<T> *>(ss + at<T, DK>(col, paired<T>(i, 4 * g)))
+                                       : *reinterpret_cast<const x4<T> *>(state + col * DK + paired<T>(i, 4 * g));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += grad[i][e] * to_float(state[(16 * i + 4 * g + e) * DV + col]);
+                for (int e = 0; e < 4; ++e) sum += grad[i][e] * to_float(s[e]);
                 grad[i] *= decay;
             }
 #pragma unroll
             for (int by = 1; by < 64; by *= 2) sum += __shfl_xor(sum, by);
-            if (lane == 0) spans[wave] = sum * decay;
+            if (lane0 == 0) spans[wave] = sum * decay;
 #pragma unroll
             for (int i = 0; i < C / 32; ++i) {
-                const Frag<T> of = load_cols(os, PV, 16 * wave, 32 * i, lane);
+                const int lane = fresh(lane0), g = lane >> 4;
+                const Frag<T> of = load_cols<DV>(os, 16 * wave, 32 * i, lane);
                 Frag<T> planes[PLANES];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float x = to_float(of[e]) * (decays.from_start[32 * i + 4 * g + (e >> 2) * 16 + (e & 3)] * p.scale);
+                    float x = to_float(of[e]) * (decays.from_start[32 * i + step_of<T>(g, e)] * p.scale);
 #pragma unroll
                     for (int j = 0; j < PLANES; ++j) {
                         planes[j][e] = (T)x;
@@ -247,14 +269,16 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 }
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    const Frag<T> qf = load_cols(qs, PK, 16 * kt, 32 * i, lane);
+                    const Frag<T> qf = load_paired<DK>(qs, kt, 32 * i, lane);
 #pragma unroll
                     for (int j = 0; j < PLANES; ++j) grad[kt] = mma(qf, planes[j], grad[kt]);
                 }
             }
         }
         __syncthreads();
-        if (wave == 0 && p.grad_log_a) { // before the next chunk's sums are written there is another barrier
+        if (wave == 0 && p.grad_log_a) {
+            const int lane = lane0;
+            // before the next chunk's sums are written there is another barrier
             double suffix = 0.0, prefix = 0.0, span = 0.0;
             if (lane < C) {
                 float x = 0.0f, y = 0.0f, across = 0.0f, below = 0.0f;
@@ -289,8 +313,8 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         for (int i = 0; i < KT; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int row = 16 * i + 4 * g + e;
-                if (row < p.K && col < p.V) to[(int64_t)row * p.V + col] = grad[i][e];
+                const int row = paired<T>(i, 4 * g + e);
+                if (row < p.K && col < p.V) to[(uint32_t)(row * p.V + col)] = grad[i][e];
             }
     }
 }
@@ -298,28 +322,27 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 // ---- few tokens -----------------------------------------------------------------------------------------------
 //
 // The recurrence and its gradients token by token in float32: s0 and grad_sn are read once, the states in between are formed
-// again for each token.  A workgroup has a head's state; a thread has VEC neighbouring columns of every ROWS-th row.
-template <typename T, int VEC>
+// again for each token.  A workgroup has a head's state; a thread has four neighbouring columns of every eighth row.
+template <typename T>
 __global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardArgs p, const float *s0)
 {
-    constexpr int ACROSS = 128 / VEC, ROWS = 256 / ACROSS, PER = 128 / ROWS, IN_WAVE = ACROSS < 64 ? ACROSS : 64, PARTS = ACROSS / IN_WAVE;
-    typedef float vec __attribute__((ext_vector_type(VEC)));
-    __shared__ float q[kFewTokens][128], k[kFewTokens][128], v[kFewTokens][128], o[kFewTokens][128], a[kFewTokens];
-    __shared__ float row_sums[2][PARTS][128], col_sums[ROWS][128], wave_sums[4];
+    constexpr int ACROSS = 32, ROWS = 256 / ACROSS, PER = 128 / ROWS;
+    __shared__ __align__(16) float q[kFewTokens][128], k[kFewTokens][128], v[kFewTokens][128], o[kFewTokens][128];
+    __shared__ float a[kFewTokens], row_sums[2][128], wave_sums[4];
+    __shared__ __align__(16) float col_sums[ROWS][128];
     const int bh = blockIdx.x, h = bh % p.H, b = bh / p.H;
-    const int row0 = threadIdx.x / ACROSS, col = threadIdx.x % ACROSS * VEC, part = threadIdx.x % ACROSS / IN_WAVE;
-    const bool inside = col < p.V;
+    const int row0 = threadIdx.x / ACROSS, col = threadIdx.x % ACROSS * 4;
     int64_t first;
     const int len = (int)sequence(p.starts, p.n, b, first);
-    const int64_t at = (int64_t)bh * p.K * p.V + col;
+    const int64_t at = (int64_t)bh * p.K * p.V;
 
-    vec start[PER], grad[PER]; // s0 and R
+    f32x4 start[PER], grad[PER]; // s0 and R
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int row = row0 + i * ROWS;
-        start[i] = grad[i] = (vec)0.0f;
-        if (s0 && inside && row < p.K) start[i] = *reinterpret_cast<const vec *>(s0 + at + (int64_t)row * p.V);
-        if (p.grad_sn && inside && row < p.K) grad[i] = *reinterpret_cast<const vec *>(p.grad_sn + at + (int64_t)row * p.V);
+        start[i] = grad[i] = f32x4{0, 0, 0, 0};
+        if (s0 && row < p.K) start[i] = load4(s0 + at + row * p.V, col, p.V);
+        if (p.grad_sn && row < p.K) grad[i] = load4(p.grad_sn + at + row * p.V, col, p.V);
     }
     for (int i = threadIdx.x; i < len * 128; i += 256) {
         const int t = i / 128, c = i % 128;
@@ -335,38 +358,30 @@ __global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardA
         }
     }
     __syncthreads();
-    auto values = [&](const float *x) {
-        vec e;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) e[i] = x[col + i];
-        return e;
-    };
+    auto values = [&](const float *x) { return *reinterpret_cast<const f32x4 *>(x + col); };
     for (int t = len - 1; t >= 0; --t) {
-        const vec vt = values(v[t]), ot = values(o[t]);
-        vec down = (vec)0.0f;
+        const f32x4 vt = values(v[t]), ot = values(o[t]);
+        f32x4 down = {0, 0, 0, 0};
         float span = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int row = row0 + i * ROWS;
-            vec s = start[i];
+            f32x4 s = start[i];
             for (int u = 0; u < t; ++u) s = s * a[u] + k[u][row] * values(v[u]);
             grad[i] += q[t][row] * ot;
-            vec dq = grad[i] * s, dk = grad[i] * vt;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) span += dq[e];
+            f32x4 dq = grad[i] * s;
+            const f32x4 dk = grad[i] * vt;
+            span += (dq[0] + dq[1]) + (dq[2] + dq[3]);
             s = s * a[t] + k[t][row] * vt;
             dq = s * ot;
             down += k[t][row] * grad[i];
-            float sum_q = 0.0f, sum_k = 0.0f;
+            float sum_q = (dq[0] + dq[1]) + (dq[2] + dq[3]), sum_k = (dk[0] + dk[1]) + (dk[2] + dk[3]);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum_q += dq[e], sum_k += dk[e];
-#pragma unroll
-            for (int by = 1; by < IN_WAVE; by *= 2) sum_q += __shfl_xor(sum_q, by), sum_k += __shfl_xor(sum_k, by);
-            if (threadIdx.x % IN_WAVE == 0) row_sums[0][part][row] = sum_q, row_sums[1][part][row] = sum_k;
+            for (int by = 1; by < ACROSS; by *= 2) sum_q += __shfl_xor(sum_q, by), sum_k += __shfl_xor(sum_k, by);
+            if (threadIdx.x % ACROSS == 0) row_sums[0][row] = sum_q, row_sums[1][row] = sum_k;
             grad[i] *= a[t];
         }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) col_sums[row0][col + e] = down[e];
+        *reinterpret_cast<f32x4 *>(&col_sums[row0][col]) = down;
 #pragma unroll
         for (int by = 1; by < 64; by *= 2) span += __shfl_xor(span, by);
         if (threadIdx.x % 64 == 0) wave_sums[threadIdx.x / 64] = span;
@@ -375,10 +390,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardA
         const int64_t token = first + t, place = ((p.share > 1 ? (int64_t)b * p.n + t : token) * p.H + h) * p.K + c;
         if (c < p.K) {
             const int which = threadIdx.x / 128;
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < PARTS; ++i) sum += row_sums[which][i][c];
-            if (which == 0) sum *= p.scale;
+            const float sum = row_sums[which][c] * (which == 0 ? p.scale : 1.0f);
             void *const to = which == 0 ? p.grad_q : p.grad_k;
             if (p.share > 1) static_cast<float *>(to)[place] = sum;
             else static_cast<T *>(to)[place] = (T)sum;
@@ -396,11 +408,11 @@ __global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardA
         }
         __syncthreads();
     }
-    if (p.grad_s0 && inside)
+    if (p.grad_s0)
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int row = row0 + i * ROWS;
-            if (row < p.K) *reinterpret_cast<vec *>(p.grad_s0 + at + (int64_t)row * p.V) = grad[i];
+            if (row < p.K) store4(p.grad_s0 + at + row * p.V, col, p.V, grad[i]);
         }
 }
 
@@ -448,11 +460,6 @@ __global__ __launch_bounds__(256) void heinsen_attention_decay_sum(const float *
 
 // ---- host -----------------------------------------------------------------------------------------------------
 
-bool rows16(const void *p, int64_t stride, int d, size_t size)
-{
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && d * size % 16 == 0;
-}
-
 template <typename T, int C, int DK, int DV> hipError_t backward_sized(const BackwardArgs &a, int64_t blocks, hipStream_t stream)
 {
     heinsen_attention_backward<T, C, DK, DV><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
@@ -463,15 +470,6 @@ template <typename T, int C> hipError_t backward(const BackwardArgs &a, int64_t 
 {
     if (a.K <= 64) return a.V <= 64 ? backward_sized<T, C, 64, 64>(a, blocks, stream) : backward_sized<T, C, 64, 128>(a, blocks, stream);
     return a.V <= 64 ? backward_sized<T, C, 128, 64>(a, blocks, stream) : backward_sized<T, C, 128, 128>(a, blocks, stream);
-}
-
-template <typename T> hipError_t step_backward(const BackwardArgs &a, const AttentionCall &c, int64_t blocks)
-{
-    bool whole = c.V % 4 == 0;
-    for (const void *p : {(const void *)c.s0, (const void *)c.grad_sn, (const void *)c.grad_s0}) whole = whole && reinterpret_cast<uintptr_t>(p) % 16 == 0;
-    if (whole) heinsen_attention_step_backward<T, 4><<<dim3((unsigned)blocks), 256, 0, c.stream>>>(a, c.s0);
-    else heinsen_attention_step_backward<T, 1><<<dim3((unsigned)blocks), 256, 0, c.stream>>>(a, c.s0);
-    return hipGetLastError();
 }
 
 // Parts of the scratch, in this order.
@@ -519,7 +517,6 @@ size_t attention_backward_scratch(const AttentionCall &c) { return parts(c).all;
 hipError_t attention_backward_launch(const AttentionCall &c, void *scratch)
 {
     const Parts s = parts(c);
-    const size_t size = c.bf16 ? 2 : 4;
     char *at = static_cast<char *>(scratch);
     float *const segment_state = reinterpret_cast<float *>(at);
     float *const segment_grad = reinterpret_cast<float *>(at += s.states);
@@ -546,14 +543,12 @@ hipError_t attention_backward_launch(const AttentionCall &c, void *scratch)
     a.n = c.n, a.q_stride = c.q_stride, a.k_stride = c.k_stride, a.v_stride = c.v_stride, a.segment = s.segments.tokens;
     a.H = c.H, a.share = c.share, a.K = c.K, a.V = c.V, a.segments = s.segments.count, a.chunks = s.chunks;
     a.scale = c.scale, a.per_head = c.per_head;
-    a.q_whole = rows16(c.q, c.q_stride, c.K, size), a.k_whole = rows16(c.k, c.k_stride, c.K, size), a.v_whole = rows16(c.v, c.v_stride, c.V, size);
-    a.out_whole = rows16(c.grad_out, (int64_t)c.H * c.V, c.V, size);
-    const size_t qk_size = c.share > 1 ? 4 : size;
-    a.grad_qk_whole = c.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.grad_q) % (4 * qk_size) == 0 && reinterpret_cast<uintptr_t>(a.grad_k) % (4 * qk_size) == 0;
-    a.grad_v_whole = c.V % 4 == 0 && reinterpret_cast<uintptr_t>(c.grad_v) % (4 * size) == 0;
     const int64_t blocks = (int64_t)c.B * c.H * s.segments.count;
-    if (few) e = c.bf16 ? step_backward<__bf16>(a, c, blocks) : step_backward<float>(a, c, blocks);
-    else e = c.bf16 ? backward<__bf16, 64>(a, blocks, c.stream) : backward<float, 32>(a, blocks, c.stream);
+    if (few) {
+        if (c.bf16) heinsen_attention_step_backward<__bf16><<<dim3((unsigned)blocks), 256, 0, c.stream>>>(a, c.s0);
+        else heinsen_attention_step_backward<float><<<dim3((unsigned)blocks), 256, 0, c.stream>>>(a, c.s0);
+        e = hipGetLastError();
+    } else e = c.bf16 ? backward<__bf16, 64>(a, blocks, c.stream) : backward<float, 32>(a, blocks, c.stream);
     if (e != hipSuccess) return e;
     return c.bf16 ? finish<__bf16>(c, shared_q, shared_k, decays) : finish<float>(c, shared_q, shared_k, decays);
 }

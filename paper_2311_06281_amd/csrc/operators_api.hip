@@ -79,12 +79,12 @@ int make_attention(const void *q, const void *k, const void *v, const void *log_
     // indexes of workgroups and chunks are 32-bit, offsets 64-bit
     const int64_t many = (int64_t)1 << 24;
     if (K > 128 || V > 128 || H > many || B > many / H || n > ((int64_t)1 << 31) || B * n > ((int64_t)1 << 36)) return HEINSEN_ERR_UNSUPPORTED;
-    const int64_t qk = Hk * K, values = H * V, most = (int64_t)1 << 24;
+    const int64_t qk = Hk * K, values = H * V, most = (int64_t)1 << 23; // 64 tokens within 32 bits of bytes
     if (q_stride == 0) q_stride = qk;
     if (k_stride == 0) k_stride = qk;
     if (v_stride == 0) v_stride = values;
     if (q_stride < qk || k_stride < qk || v_stride < values) return HEINSEN_ERR_INVALID_ARG;
-    if (q_stride > most * 64 || k_stride > most * 64 || v_stride > most * 64) return HEINSEN_ERR_UNSUPPORTED;
+    if (q_stride > most || k_stride > most || v_stride > most) return HEINSEN_ERR_UNSUPPORTED;
     c.q = q, c.k = k, c.v = v, c.log_a = log_a;
     c.s0 = static_cast<const float *>(s0);
     c.starts = static_cast<const int64_t *>(starts);
