@@ -107,6 +107,57 @@ template <int D, typename T> __device__ static inline Frag<T> load_paired(const 
     return columns<D>(tile, paired<T>(block, 0), sizeof(T) == 2 ? 8 : 4, k0, lane);
 }
 
+// Eight float32 in the fragment's order of steps, from k0 on.
+template <typename T> __device__ static inline f32x8 load_steps(const float *p, int g)
+{
+    const f32x4 *const at = reinterpret_cast<const f32x4 *>(p + (sizeof(T) == 2 ? 8 : 4) * g);
+    return __builtin_shufflevector(at[0], at[sizeof(T) == 2 ? 1 : 4], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The float32 numbers of a fragment.
+__device__ static inline f32x8 widen(bf16x8 f)
+{
+    const u32x4 u = __builtin_bit_cast(u32x4, f);
+    f32x8 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+        x[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+    }
+    return x;
+}
+__device__ static inline f32x8 widen(f32x8 f) { return f; }
+
+// x as the sum of fragments: three bfloat16 numbers hold the 24 bits of a float32.  `odd`: an infinite entry may be there,
+// which leaves nothing over.
+template <typename T> struct Split;
+template <> struct Split<float> {
+    static constexpr int COUNT = 1;
+    f32x8 part[1];
+    __device__ void set(f32x8 x, bool) { part[0] = x; }
+};
+template <> struct Split<__bf16> {
+    static constexpr int COUNT = 3;
+    bf16x8 part[3];
+    __device__ void set(f32x8 x, bool odd)
+    {
+        part[0] = __builtin_convertvector(x, bf16x8);
+        x -= widen(part[0]);
+        part[1] = __builtin_convertvector(x, bf16x8);
+        x -= widen(part[1]);
+        part[2] = __builtin_convertvector(x, bf16x8);
+        if (odd) {
+            const u32x4 u = __builtin_bit_cast(u32x4, part[0]);
+            u32x4 keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                keep[i] = ((u[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u) | ((u[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu);
+            part[1] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, part[1]) & keep);
+            part[2] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, part[2]) & keep);
+        }
+    }
+};
+
 // ---- rows in global memory --------------------------------------------------------------------------------
 //
 // Rows start wherever their type may: the accesses are of 16 (stores: 8 or 16) bytes all the same, which the memory pipeline
@@ -122,58 +173,57 @@ template <> struct Unaligned<__bf16> {
     typedef bf16x4 __attribute__((aligned(2))) vec4;
 };
 
+#define AS_GLOBAL __attribute__((address_space(1)))
+
+static __device__ const uint32_t kNothing[4] = {0, 0, 0, 0}; // something to read where there is nothing
+
 // A tile of C rows of D entries on its way from global memory to LDS, in registers.
 template <typename T, int C, int D, int THREADS> struct TileLoad {
     static constexpr int N = 16 / (int)sizeof(T);
     static constexpr int PER_ROW = D / N;
-    static constexpr int COUNT = C * PER_ROW / THREADS;
-    static_assert(C * PER_ROW % THREADS == 0 && THREADS % PER_ROW == 0, "whole rounds of whole rows");
+    static constexpr int AT_ONCE = THREADS / PER_ROW; // rows
+    static constexpr int COUNT = C / AT_ONCE;
+    static_assert(C % AT_ONCE == 0 && THREADS % PER_ROW == 0, "whole rounds of whole rows");
     u32x4 v[COUNT];
+    const char AS_GLOBAL *next; // the first row of the next tile
+    uint32_t step, offset;      // bytes from row to row; from `next` to this thread's first piece
 
     __device__ static int col() { return threadIdx.x % PER_ROW * N; }
-    __device__ static int row(int i) { return threadIdx.x / PER_ROW + i * (THREADS / PER_ROW); }
+    __device__ static int row(int i) { return threadIdx.x / PER_ROW + i * AT_ONCE; }
 
-    // rows 0..rows-1 start at base + row * stride and have d entries: the others and the rest of each are read from where
-    // there are some
-    __device__ void load(const T *base, int64_t stride, int rows, int d)
+    // Rows of d entries start at base + row * stride.  Where a row ends within a piece or before it, the last whole vector of
+    // the row is read.  Rows shorter than a vector are left to store().
+    __device__ void start(const T *base, int64_t stride, int d)
     {
-        if (d < N) { // too few for a vector
+        next = (const char AS_GLOBAL *)(d < N ? reinterpret_cast<uintptr_t>(kNothing) : reinterpret_cast<uintptr_t>(base));
+        step = d < N ? 0 : (uint32_t)stride * (uint32_t)sizeof(T);
+        offset = row(0) * step + (d < N ? 0 : (col() < d - N ? col() : d - N) * (uint32_t)sizeof(T));
+    }
+    // rows past the last are read from it
+    __device__ void load(int rows)
+    {
+        if (rows == C) {
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) {
-                typedef T vec __attribute__((ext_vector_type(N)));
-                const T *const from = base + (row(i) < rows ? row(i) : rows - 1) * stride;
-                vec e;
+            for (int i = 0; i < COUNT; ++i) v[i] = *(const typename Unaligned<T>::vec16 AS_GLOBAL *)(next + (uint64_t)step * (i * AT_ONCE) + offset);
+        } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) e[j] = from[j < d ? j : 0];
-                v[i] = __builtin_bit_cast(u32x4, e);
-            }
-            return;
-        }
-        const uint32_t first = (col() < d - N ? col() : d - N) * (uint32_t)sizeof(T), step = (uint32_t)stride * (uint32_t)sizeof(T);
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            const uint32_t offset = (uint32_t)(row(i) < rows ? row(i) : rows - 1) * step + first;
-            v[i] = *reinterpret_cast<const typename Unaligned<T>::vec16 *>(reinterpret_cast<const char *>(base) + offset);
+            for (int i = 0; i < COUNT; ++i)
+                v[i] = *(const typename Unaligned<T>::vec16 AS_GLOBAL *)(next + (offset + ((row(i) < rows ? row(i) : rows - 1) - row(0)) * step));
         }
     }
-    // puts what was read in place: entries from the d-th on and rows from `rows` on are zero
+    __device__ void move(int rows) { next += (int64_t)rows * (int64_t)step; }
+    // Puts what was read in place: entries from the d-th on and rows from `rows` on are zero.
     __device__ void settle(int rows, int d)
     {
-        if (d < D) {
-            const int from = d < N ? 0 : col() < d - N ? col() : d - N; // the first entry read
-            const int shift = (col() - from) * 8 * (int)sizeof(T), keep = d - col() < N ? d - col() : N;
+        if (d < D && d >= N) {
+            const int shift = (col() - (col() < d - N ? col() : d - N)) * 8 * (int)sizeof(T);
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const uint64_t lo = ((uint64_t)v[i][1] << 32) | v[i][0], hi = ((uint64_t)v[i][3] << 32) | v[i][2];
                 uint64_t a = shift >= 64 ? hi : lo, b = shift >= 64 ? 0 : hi;
                 a = (a >> (shift & 63)) | ((b << 1) << (63 - (shift & 63)));
                 b >>= shift & 63;
-                if (d < N && keep > 0) { // entries read in the place of others
-                    const int bits = keep * 8 * (int)sizeof(T);
-                    a = bits >= 64 ? a : a & (((uint64_t)1 << bits) - 1);
-                    b = bits > 64 ? b & (((uint64_t)1 << (bits - 64)) - 1) : 0;
-                }
-                if (keep <= 0) a = b = 0;
+                if (shift >= 128) a = 0;
                 v[i] = u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
             }
         }
@@ -182,22 +232,35 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
             for (int i = 0; i < COUNT; ++i)
                 if (row(i) >= rows) v[i] = u32x4{0, 0, 0, 0};
     }
-    __device__ void store(T *tile) const
+    // Returns whether a row shorter than a vector has an infinite or NaN entry.
+    __device__ bool store(T *tile, const T *base, int64_t stride, int rows, int d) const
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) *reinterpret_cast<u32x4 *>(tile + at<T, D>(row(i), col())) = v[i];
+        bool odd = false;
+        if (d < N && col() == 0) {
+#pragma unroll 1
+            for (int at_row = row(0); at_row < rows; at_row += THREADS / PER_ROW)
+#pragma unroll 1
+                for (int j = 0; j < d; ++j) {
+                    const T x = base[at_row * stride + j];
+                    tile[at<T, D>(at_row, j)] = x;
+                    odd |= !(__builtin_fabsf((float)x) < __builtin_inff());
+                }
+        }
+        return odd;
     }
     // whether an entry is infinite or NaN
     __device__ bool not_finite() const
     {
+        // adding one to an exponent of ones carries into the sign
+        constexpr uint32_t EXPONENTS = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, ONE = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
         uint32_t bad = 0;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                bad |= (uint32_t)((v[i][j] & 0x7f800000u) == 0x7f800000u);
-                if (sizeof(T) == 2) bad |= (uint32_t)((v[i][j] & 0x7f80u) == 0x7f80u);
-            }
+            for (int j = 0; j < 4; ++j) bad |= (v[i][j] & EXPONENTS) + ONE;
+        bad &= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
         return bad != 0;
     }
 };
@@ -237,11 +300,24 @@ template <int C> struct Decays {
     float total;             // 2^G_C
 };
 
-__device__ static inline double lane_up(double x, int by)
+// x of the lane `CTRL` (a data-parallel primitive's shift or broadcast) says in the rows of MASK, zero where there is none
+template <int CTRL, int MASK = 0xf> __device__ static inline double moved(double x)
 {
     const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __shfl_up((uint32_t)u, by), hi = __shfl_up((uint32_t)(u >> 32), by);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, MASK, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, MASK, 0xf, false);
     return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+// sum of x over the lanes up to this one
+__device__ static inline double prefix_sum(double x)
+{
+    x += moved<0x111>(x); // by 1, 2, 4, 8 within rows of sixteen lanes
+    x += moved<0x112>(x);
+    x += moved<0x114>(x);
+    x += moved<0x118>(x);
+    x += moved<0x142, 0xa>(x); // the first and third row's sum to the next one, then the first half's to the second
+    x += moved<0x143, 0xc>(x);
+    return x;
 }
 __device__ static inline double lane_at(double x, int lane)
 {
@@ -257,11 +333,7 @@ template <int C> __device__ static inline double write_decays(Decays<C> &d, floa
     if (log_a <= -104.0f) g = -4096.0; // exp(-104) is zero in float32, subnormal numbers included
     if (log_a >= 2840.0f) g = 4096.0;
     if (lane >= C) g = 0.0;
-#pragma unroll
-    for (int by = 1; by < C; by *= 2) {
-        const double other = lane_up(g, by);
-        if (lane >= by) g += other;
-    }
+    g = prefix_sum(g);
     const double end = lane_at(g, C - 1);
     if (lane < C) {
         const double w = floor(g);

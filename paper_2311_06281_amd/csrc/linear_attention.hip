@@ -55,8 +55,6 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
 {
     constexpr int KT = DK / 16, NT = DV / 16 / kWaves, TT = C / 16;
     constexpr bool BACK = SWEEP == kSegmentGradient;
-    // v scaled by its decay is summed into the state as the sum of this many bfloat16 numbers: three hold 24 bits
-    constexpr int PLANES = sizeof(T) == 4 ? 1 : 3;
     __shared__ __align__(16) T ks[C * DK];
     __shared__ __align__(16) T vs[C * DV];
     __shared__ __align__(16) T qs[SWEEP == kOutput ? C * DK : 16];
@@ -109,12 +107,20 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
     TileLoad<T, C, DK, kThreads> next_q, next_k;
     TileLoad<T, C, DV, kThreads> next_v;
     T next_log_a = (T)0.0f;
+    next_k.start(k + chunk_start(0) * p.k_stride, p.k_stride, p.K);
+    next_v.start(v + chunk_start(0) * p.v_stride, p.v_stride, V);
+    if (SWEEP == kOutput) next_q.start(q + chunk_start(0) * p.q_stride, p.q_stride, p.K);
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K);
-        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, V);
-        if (SWEEP == kOutput) next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K);
-        if (log_a) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
+        next_k.load(rows);
+        next_k.move(BACK ? -C : C);
+        next_v.load(rows);
+        next_v.move(BACK ? -C : C);
+        if (SWEEP == kOutput) {
+            next_q.load(rows);
+            next_q.move(C);
+        }
+        if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
     };
     if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
     if (chunks > 0) request(chunk_start(0));
@@ -124,14 +130,14 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
         const int64_t t0 = chunk_start(chunk);
         const int rows = (int)(end - t0 < C ? end - t0 : C);
         next_k.settle(rows, p.K);
-        next_k.store(ks);
+        next_k.store(ks, k + t0 * p.k_stride, p.k_stride, rows, p.K);
         next_v.settle(rows, V);
-        next_v.store(vs);
+        const bool odd = next_v.store(vs, v + t0 * p.v_stride, p.v_stride, rows, V);
         if (SWEEP == kOutput) {
             next_q.settle(rows, p.K);
-            next_q.store(qs);
+            next_q.store(qs, q + t0 * p.q_stride, p.q_stride, rows, p.K);
         }
-        if (next_v.not_finite()) atomicOr(&not_finite[chunk & 1], 1);
+        if (next_v.not_finite() || odd) atomicOr(&not_finite[chunk & 1], 1);
         if (wave == 0) total += write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
         __syncthreads();
         const bool odd_values = not_finite[chunk & 1] != 0;
@@ -174,10 +180,13 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
         }
 
         Frag<T> vf[C / 32][NT];
+        {
+            const int lane = fresh(lane0);
 #pragma unroll
-        for (int i = 0; i < C / 32; ++i)
+            for (int i = 0; i < C / 32; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) vf[i][j] = load_values(vs, j, 32 * i, fresh(lane0));
+                for (int j = 0; j < NT; ++j) vf[i][j] = load_values(vs, j, 32 * i, lane);
+        }
 
         if (SWEEP == kOutput) {
             if (odd_values)
@@ -247,46 +256,39 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
         for (int i = 0; i < KT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) state[i][j] *= decay;
+        const int lane = fresh(lane0);
 #pragma unroll
         for (int i = 0; i < C / 32; ++i) {
-            const int lane = fresh(lane0), g = lane >> 4;
-            const float *const w = (BACK ? decays.from_start : decays.to_end) + 32 * i;
-            Frag<T> vw[NT][PLANES];
+            f32x8 w = load_steps<T>((BACK ? decays.from_start : decays.to_end) + 32 * i, lane >> 4);
+            if (BACK) w *= p.scale;
+            // v scaled by its decay enters unrounded
+            Split<T> vw[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = to_float(vf[i][j][e]) * w[step_of<T>(g, e)];
-                    if (BACK) x *= p.scale;
-#pragma unroll
-                    for (int plane = 0; plane < PLANES; ++plane) {
-                        const T part = (T)x;
-                        vw[j][plane][e] = part;
-                        x -= to_float(part);
-                        if (PLANES > 1 && odd_values && !(__builtin_fabsf(to_float(part)) < __builtin_inff())) x = 0.0f;
-                    }
-                }
+            for (int j = 0; j < NT; ++j) vw[j].set(widen(vf[i][j]) * w, odd_values);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
                 const Frag<T> kf = load_paired<DK>(ks, kt, 32 * i, lane);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int plane = 0; plane < PLANES; ++plane) state[kt][j] = mma(kf, vw[j][plane], state[kt][j]);
+                    for (int e = 0; e < Split<T>::COUNT; ++e) state[kt][j] = mma(kf, vw[j].part[e], state[kt][j]);
             }
         }
         // rows past the K-th stay zero, also where zero was multiplied by infinity
-        if (odd_values || !(__builtin_fabsf(decay) < __builtin_inff()))
+        if (odd_values || !(__builtin_fabsf(decay) < __builtin_inff())) {
+            const int g = fresh(lane0) >> 4;
 #pragma unroll
             for (int i = 0; i < KT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+                for (int e = 0; e < 4; ++e)
+                    if (paired<T>(i, 4 * g + e) >= p.K)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (paired<T>(i, 4 * g + e) >= p.K) state[i][j][e] = 0.0f;
+                        for (int j = 0; j < NT; ++j) state[i][j][e] = 0.0f;
+        }
         __syncthreads();
     }
 
+    const int row0 = fresh(4 * g), col0 = fresh(r);
     float *to = nullptr;
     if (SWEEP == kSegmentState || SWEEP == kSegmentGradient) {
         to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0;
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int row = paired<T>(i, 4 * g + e), c = column(j, r);
+                    const int row = paired<T>(i, row0 + e), c = column(j, col0);
                     if (row < p.K && c < V) to[(uint32_t)(row * p.V + c)] = state[i][j][e];
                 }
 }

@@ -39,7 +39,6 @@ template <typename T, int C, int DK, int DV>
 __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(BackwardArgs p)
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
-    constexpr int PLANES = sizeof(T) == 4 ? 1 : 3; // of q do^T's operand, see heinsen_attention_sweep
     constexpr bool STAGED = sizeof(T) == 2;        // the chunk's first state goes through LDS; in float32 there is no room
     __shared__ __align__(16) T qs[C * DK];
     __shared__ __align__(16) T ks[C * DK];
@@ -88,29 +87,42 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     TileLoad<T, STAGED ? DV : THREADS * 16 / (int)sizeof(T) / DK, DK, THREADS> next_s;
     T next_log_a = (T)0.0f;
     auto state_of = [&](int64_t t0) { return static_cast<const T *>(p.states) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV); };
+    const int64_t last = begin + (int64_t)(chunks - 1) * C; // the last chunk's first token
+    next_q.start(q + last * p.q_stride, p.q_stride, p.K);
+    next_k.start(k + last * p.k_stride, p.k_stride, p.K);
+    next_v.start(v + last * p.v_stride, p.v_stride, p.V);
+    next_o.start(o + last * o_stride, o_stride, p.V);
+    if (STAGED) next_s.start(state_of(last), DK, DK);
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_q.load(q + t0 * p.q_stride, p.q_stride, rows, p.K);
-        next_k.load(k + t0 * p.k_stride, p.k_stride, rows, p.K);
-        next_v.load(v + t0 * p.v_stride, p.v_stride, rows, p.V);
-        next_o.load(o + t0 * o_stride, o_stride, rows, p.V);
-        if (STAGED) next_s.load(state_of(t0), DK, DV, DK);
-        if (log_a) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
+        next_q.load(rows);
+        next_q.move(-C);
+        next_k.load(rows);
+        next_k.move(-C);
+        next_v.load(rows);
+        next_v.move(-C);
+        next_o.load(rows);
+        next_o.move(-C);
+        if (STAGED) {
+            next_s.load(DV);
+            next_s.move(-DV);
+        }
+        if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
     };
-    if (chunks > 0) request(begin + (int64_t)(chunks - 1) * C);
+    if (chunks > 0) request(last);
 
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
         const int64_t t0 = begin + (int64_t)chunk * C;
         const int rows = (int)(end - t0 < C ? end - t0 : C);
         next_q.settle(rows, p.K);
-        next_q.store(qs);
+        next_q.store(qs, q + t0 * p.q_stride, p.q_stride, rows, p.K);
         next_k.settle(rows, p.K);
-        next_k.store(ks);
+        next_k.store(ks, k + t0 * p.k_stride, p.k_stride, rows, p.K);
         next_v.settle(rows, p.V);
-        next_v.store(vs);
+        next_v.store(vs, v + t0 * p.v_stride, p.v_stride, rows, p.V);
         next_o.settle(rows, p.V);
-        next_o.store(os);
-        if (STAGED) next_s.store(ss);
+        next_o.store(os, o + t0 * o_stride, o_stride, rows, p.V);
+        if (STAGED) next_s.store(ss, state_of(t0), DK, DV, DK);
         if (wave == 0) write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
 #pragma unroll
         for (int i = 0; i < KT; ++i)
@@ -257,21 +269,14 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             for (int i = 0; i < C / 32; ++i) {
                 const int lane = fresh(lane0), g = lane >> 4;
                 const Frag<T> of = load_cols<DV>(os, 16 * wave, 32 * i, lane);
-                Frag<T> planes[PLANES];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = to_float(of[e]) * (decays.from_start[32 * i + step_of<T>(g, e)] * p.scale);
-#pragma unroll
-                    for (int j = 0; j < PLANES; ++j) {
-                        planes[j][e] = (T)x;
-                        x -= to_float(planes[j][e]);
-                    }
-                }
+                const f32x8 w = load_steps<T>(decays.from_start + 32 * i, g) * p.scale;
+                Split<T> ow;
+                ow.set(widen(of) * w, false);
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
                     const Frag<T> qf = load_paired<DK>(qs, kt, 32 * i, lane);
 #pragma unroll
-                    for (int j = 0; j < PLANES; ++j) grad[kt] = mma(qf, planes[j], grad[kt]);
+                    for (int e = 0; e < Split<T>::COUNT; ++e) grad[kt] = mma(qf, ow.part[e], grad[kt]);
                 }
             }
         }
@@ -292,15 +297,10 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             }
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) span += spans[i];
-            const double own = prefix;
-#pragma unroll
-            for (int by = 1; by < C; by *= 2) {
-                const double up = lane_up(prefix, by), down = lane_at(suffix, (lane + by) & 63);
-                if (lane >= by) prefix += up;
-                if (lane + by < C) suffix += down;
-            }
+            // of x and the pairs from this token on, of y before it
+            const double upto = prefix_sum(suffix), from = lane_at(upto, 63) - upto + suffix, before = prefix_sum(prefix) - prefix;
             if (lane < rows) {
-                const float sum = (float)(suffix + (prefix - own) + span);
+                const float sum = (float)(from + before + span);
                 if (p.per_head) static_cast<float *>(p.grad_log_a)[(b * p.n + t0 + lane) * p.H + h] = sum;
                 else static_cast<T *>(p.grad_log_a)[(first + t0 + lane) * p.H + h] = (T)sum;
             }
