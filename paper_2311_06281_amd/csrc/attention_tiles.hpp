@@ -158,6 +158,18 @@ template <> struct Split<__bf16> {
     }
 };
 
+// x, of which the compiler does not know that it is: what is formed from it is formed here, not ahead of the loop, where the
+// addresses of all the accesses of a chunk would fill the registers.
+__device__ static inline int fresh(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// x, the same in all lanes, in scalar registers
+__device__ static inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ static inline uint64_t uniform(uint64_t x) { return ((uint64_t)uniform((uint32_t)(x >> 32)) << 32) | uniform((uint32_t)x); }
+
 // ---- rows in global memory --------------------------------------------------------------------------------
 //
 // Rows start wherever their type may: the accesses are of 16 (stores: 8 or 16) bytes all the same, which the memory pipeline
@@ -175,8 +187,6 @@ template <> struct Unaligned<__bf16> {
 
 #define AS_GLOBAL __attribute__((address_space(1)))
 
-static __device__ const uint32_t kNothing[4] = {0, 0, 0, 0}; // something to read where there is nothing
-
 // A tile of C rows of D entries on its way from global memory to LDS, in registers.
 template <typename T, int C, int D, int THREADS> struct TileLoad {
     static constexpr int N = 16 / (int)sizeof(T);
@@ -185,8 +195,8 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
     static constexpr int COUNT = C / AT_ONCE;
     static_assert(C % AT_ONCE == 0 && THREADS % PER_ROW == 0, "whole rounds of whole rows");
     u32x4 v[COUNT];
-    const char AS_GLOBAL *next; // the first row of the next tile
-    uint32_t step, offset;      // bytes from row to row; from `next` to this thread's first piece
+    uint64_t next;      // address of the next tile's first row
+    uint32_t step, end; // bytes from row to row, and of a row (none: too short for a vector)
 
     __device__ static int col() { return threadIdx.x % PER_ROW * N; }
     __device__ static int row(int i) { return threadIdx.x / PER_ROW + i * AT_ONCE; }
@@ -195,28 +205,26 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
     // the row is read.  Rows shorter than a vector are left to store().
     __device__ void start(const T *base, int64_t stride, int d)
     {
-        next = (const char AS_GLOBAL *)(d < N ? reinterpret_cast<uintptr_t>(kNothing) : reinterpret_cast<uintptr_t>(base));
-        step = d < N ? 0 : (uint32_t)stride * (uint32_t)sizeof(T);
-        offset = row(0) * step + (d < N ? 0 : (col() < d - N ? col() : d - N) * (uint32_t)sizeof(T));
+        next = uniform((uint64_t)reinterpret_cast<uintptr_t>(base));
+        step = uniform((uint32_t)stride * (uint32_t)sizeof(T));
+        end = d < N ? 0 : (uint32_t)d * (uint32_t)sizeof(T);
     }
-    // rows past the last are read from it
+    // Rows past the last are zero: the hardware reads nothing past the end that it is told.
     __device__ void load(int rows)
     {
-        if (rows == C) {
+        const uint32_t thread = (uint32_t)fresh((int)threadIdx.x), piece = thread % PER_ROW * 16, last = end - 16;
+        const uint32_t offset = thread / PER_ROW * step + (piece < last ? piece : last);
+        const __amdgpu_buffer_rsrc_t memory =
+            __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(next), 0, end == 0 ? 0 : (int)((uint32_t)(rows - 1) * step + end), 0x00020000);
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) v[i] = *(const typename Unaligned<T>::vec16 AS_GLOBAL *)(next + (uint64_t)step * (i * AT_ONCE) + offset);
-        } else {
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i)
-                v[i] = *(const typename Unaligned<T>::vec16 AS_GLOBAL *)(next + (offset + ((row(i) < rows ? row(i) : rows - 1) - row(0)) * step));
-        }
+        for (int i = 0; i < COUNT; ++i) v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(memory, (int)offset, (int)(step * (i * AT_ONCE)), 0));
     }
-    __device__ void move(int rows) { next += (int64_t)rows * (int64_t)step; }
-    // Puts what was read in place: entries from the d-th on and rows from `rows` on are zero.
-    __device__ void settle(int rows, int d)
+    __device__ void move(int rows) { next += (uint64_t)((int64_t)rows * (int64_t)step); }
+    // Puts what was read of a row's last piece in place: entries from the d-th on are zero.
+    __device__ void settle(int d)
     {
         if (d < D && d >= N) {
-            const int shift = (col() - (col() < d - N ? col() : d - N)) * 8 * (int)sizeof(T);
+            const int col = fresh(this->col()), shift = (col - (col < d - N ? col : d - N)) * 8 * (int)sizeof(T);
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const uint64_t lo = ((uint64_t)v[i][1] << 32) | v[i][0], hi = ((uint64_t)v[i][3] << 32) | v[i][2];
@@ -227,10 +235,6 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
                 v[i] = u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
             }
         }
-        if (rows < C)
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i)
-                if (row(i) >= rows) v[i] = u32x4{0, 0, 0, 0};
     }
     // Returns whether a row shorter than a vector has an infinite or NaN entry.
     __device__ bool store(T *tile, const T *base, int64_t stride, int rows, int d) const
@@ -240,7 +244,7 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
         bool odd = false;
         if (d < N && col() == 0) {
 #pragma unroll 1
-            for (int at_row = row(0); at_row < rows; at_row += THREADS / PER_ROW)
+            for (int at_row = fresh(row(0)); at_row < rows; at_row += THREADS / PER_ROW)
 #pragma unroll 1
                 for (int j = 0; j < d; ++j) {
                     const T x = base[at_row * stride + j];
@@ -277,15 +281,17 @@ __device__ static inline f32x4 load4(const float *row, int col, int d)
     return v;
 }
 
-// four entries from `col` on of a row of d entries
-template <typename T> __device__ static inline void store4(T *row, int col, int d, f32x4 v)
+// four entries of a row of d entries from `col` on; the row starts `row` entries behind `base`, the same in all lanes
+template <typename T> __device__ static inline void store4(T *base, uint32_t row, int col, int d, f32x4 v)
 {
+    char AS_GLOBAL *const to = (char AS_GLOBAL *)(uintptr_t)base;
+    const uint32_t offset = (row + (uint32_t)col) * (uint32_t)sizeof(T);
     const x4<T> e = __builtin_convertvector(v, x4<T>);
-    if (col + 4 <= d) *reinterpret_cast<typename Unaligned<T>::vec4 *>(row + col) = e;
+    if (col + 4 <= d) *(typename Unaligned<T>::vec4 AS_GLOBAL *)(to + offset) = e;
     else
 #pragma unroll
         for (int i = 0; i < 3; ++i)
-            if (col + i < d) row[col + i] = e[i];
+            if (col + i < d) *(T AS_GLOBAL *)(to + offset + i * (uint32_t)sizeof(T)) = e[i];
 }
 
 // ---- decays within a chunk ------------------------------------------------------------------------------------
@@ -319,22 +325,24 @@ __device__ static inline double prefix_sum(double x)
     x += moved<0x143, 0xc>(x);
     return x;
 }
-__device__ static inline double lane_at(double x, int lane)
+// x of one lane
+__device__ static inline double of_lane(double x, int lane)
 {
     const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __shfl((uint32_t)u, lane), hi = __shfl((uint32_t)(u >> 32), lane);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
     return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 
 // One wave: lane t has log a_t (natural), zero after the last token.  Returns log2 of the chunk's decay.
 template <int C> __device__ static inline double write_decays(Decays<C> &d, float log_a, int lane)
 {
+    lane = fresh(lane);
     double g = (double)log_a * 1.4426950408889634;
     if (log_a <= -104.0f) g = -4096.0; // exp(-104) is zero in float32, subnormal numbers included
     if (log_a >= 2840.0f) g = 4096.0;
     if (lane >= C) g = 0.0;
     g = prefix_sum(g);
-    const double end = lane_at(g, C - 1);
+    const double end = of_lane(g, C - 1);
     if (lane < C) {
         const double w = floor(g);
         d.whole[lane] = (float)w;
@@ -344,14 +352,6 @@ template <int C> __device__ static inline double write_decays(Decays<C> &d, floa
         if (lane == 0) d.total = __builtin_amdgcn_exp2f((float)end);
     }
     return end;
-}
-
-// x, of which the compiler does not know that it is: what is formed from it is formed here, not ahead of the loop, where the
-// addresses of all the accesses of a chunk would fill the registers.
-__device__ static inline int fresh(int x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
 }
 
 template <typename T> __device__ static inline float to_float(T x) { return (float)x; }
@@ -366,6 +366,14 @@ __device__ static inline int64_t sequence(const int64_t *starts, int64_t n, int 
     first = starts[b];
     const int64_t len = starts[b + 1] - first;
     return len < 0 ? 0 : len < n ? len : n;
+}
+// the same where all lanes ask for one b
+__device__ static inline int64_t uniform_sequence(const int64_t *starts, int64_t n, int b, int64_t &first)
+{
+    int64_t at;
+    const int64_t len = sequence(starts, n, b, at);
+    first = (int64_t)uniform((uint64_t)at);
+    return (int64_t)uniform((uint64_t)len);
 }
 
 } // namespace hs

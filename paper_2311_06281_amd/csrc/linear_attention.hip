@@ -7,11 +7,10 @@
 //     o_t = scale (e^{G_t} S^T q_t + sum_{s<=t} e^{G_t-G_s} (q_t . k_s) v_s),   S' = e^{G_C} S + sum_s e^{G_C-G_s} k_s v_s^T.
 #include "attention_tiles.hpp"
 #include "operators.hpp"
+#include <cstdlib>
 
 namespace hs {
 namespace {
-
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 enum Sweep { kOutput, kSegmentState, kSegmentGradient, kChunkStates };
 
@@ -47,13 +46,13 @@ __device__ static inline int unit_and_slice(int slices, int &slice)
     return blockIdx.x / (8 * slices) * 8 + blockIdx.x % 8;
 }
 
-// A workgroup takes one segment of one head's tokens and goes through its chunks, DV columns of the state in registers: each
-// wave has a quarter of them.  kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
+// A workgroup takes one segment of one head's tokens and goes through its chunks, DV columns of the state in registers, sixteen
+// to a wave.  kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
 // (k, v) and gives the segment's own part of the gradient of the state it starts from.
 template <typename T, int C, int DK, int DV, int SWEEP>
-__global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs p)
+__global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p)
 {
-    constexpr int KT = DK / 16, NT = DV / 16 / kWaves, TT = C / 16;
+    constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
     constexpr bool BACK = SWEEP == kSegmentGradient;
     __shared__ __align__(16) T ks[C * DK];
     __shared__ __align__(16) T vs[C * DV];
@@ -62,13 +61,13 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
     __shared__ Decays<C> decays;
     __shared__ int not_finite[2]; // of even and odd chunks
 
-    const int lane0 = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane0 & 15, g = lane0 >> 4;
+    const int lane0 = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), r = lane0 & 15, g = lane0 >> 4;
     int slice;
     const int unit = unit_and_slice(p.slices, slice);
     if (unit >= p.units) return;
     const int seg = unit % p.segments, bh = unit / p.segments, h = bh % p.H, b = bh / p.H;
     int64_t first;
-    const int64_t len = sequence(p.starts, p.n, b, first);
+    const int64_t len = uniform_sequence(p.starts, p.n, b, first);
     const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
     if (begin >= len && (seg > 0 || SWEEP != kOutput)) return;
 
@@ -77,35 +76,29 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
     const T *const q = static_cast<const T *>(p.q) + first * p.q_stride + (int64_t)(h / p.share) * p.K;
     const T *const v = static_cast<const T *>(p.v) + first * p.v_stride + (int64_t)h * p.V + v0;
     const T *const log_a = static_cast<const T *>(p.log_a);
-    // the column of v that row or column r of this wave's block j stands for
-    auto column = [&](int j, int r) { return NT > 1 ? paired<T>(wave * NT + j, r) : 16 * wave + r; };
-    auto load_values = [&](const T *tile, int j, int k0, int lane) {
-        return NT > 1 ? load_paired<DV>(tile, wave * NT + j, k0, lane) : load_cols<DV>(tile, 16 * wave, k0, lane);
-    };
+    const int col = 16 * wave + r; // of v, of this lane's entries of the state
 
-    f32x4 state[KT][NT];
+    f32x4 state[KT];
     const bool segment_start = (SWEEP == kOutput || SWEEP == kChunkStates) && p.segments > 1 && begin < len;
     const float *const from = segment_start ? p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0
                               : (SWEEP == kOutput || SWEEP == kChunkStates) && p.s0 ? p.s0 + (int64_t)bh * p.K * p.V + v0 : nullptr;
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
+    for (int i = 0; i < KT; ++i) {
+        state[i] = f32x4{0, 0, 0, 0};
+        if (from)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            state[i][j] = f32x4{0, 0, 0, 0};
-            if (from)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = paired<T>(i, 4 * g + e), c = column(j, r);
-                    const float x = from[(uint32_t)((row < p.K ? row : 0) * p.V + (c < V ? c : 0))];
-                    state[i][j][e] = row < p.K && c < V ? x : 0.0f;
-                }
-        }
+            for (int e = 0; e < 4; ++e) {
+                const int row = paired<T>(i, 4 * g + e);
+                const float x = from[(uint32_t)((row < p.K ? row : 0) * p.V + (col < V ? col : 0))];
+                state[i][e] = row < p.K && col < V ? x : 0.0f;
+            }
+    }
     double total = 0.0; // log2 of the decay so far (wave 0)
 
     const int chunks = (int)((end - begin + C - 1) / C);
     auto chunk_start = [&](int i) { return begin + (int64_t)(BACK ? chunks - 1 - i : i) * C; };
-    TileLoad<T, C, DK, kThreads> next_q, next_k;
-    TileLoad<T, C, DV, kThreads> next_v;
+    TileLoad<T, C, DK, THREADS> next_q, next_k;
+    TileLoad<T, C, DV, THREADS> next_v;
     T next_log_a = (T)0.0f;
     next_k.start(k + chunk_start(0) * p.k_stride, p.k_stride, p.K);
     next_v.start(v + chunk_start(0) * p.v_stride, p.v_stride, V);
@@ -120,7 +113,7 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
             next_q.load(rows);
             next_q.move(C);
         }
-        if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
+        if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + fresh(lane0 < rows ? lane0 : 0)) * p.H + h];
     };
     if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
     if (chunks > 0) request(chunk_start(0));
@@ -129,16 +122,19 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int64_t t0 = chunk_start(chunk);
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_k.settle(rows, p.K);
+        next_k.settle(p.K);
         next_k.store(ks, k + t0 * p.k_stride, p.k_stride, rows, p.K);
-        next_v.settle(rows, V);
+        next_v.settle(V);
         const bool odd = next_v.store(vs, v + t0 * p.v_stride, p.v_stride, rows, V);
         if (SWEEP == kOutput) {
-            next_q.settle(rows, p.K);
+            next_q.settle(p.K);
             next_q.store(qs, q + t0 * p.q_stride, p.q_stride, rows, p.K);
         }
         if (next_v.not_finite() || odd) atomicOr(&not_finite[chunk & 1], 1);
-        if (wave == 0) total += write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
+        if (wave == 0) {
+            const double chunk_total = write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
+            if (SWEEP == kSegmentState || BACK) total += chunk_total;
+        }
         __syncthreads();
         const bool odd_values = not_finite[chunk & 1] != 0;
         if (threadIdx.x == 0) not_finite[(chunk + 1) & 1] = 0;
@@ -153,7 +149,7 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
 #pragma unroll
             for (int i = 0; i < DK / 32; ++i) qf[i] = load_rows<DK>(qs, 16 * tt, 32 * i, lane);
             const float whole_t = decays.whole[16 * tt + r], part_t = decays.part[16 * tt + r];
-            for (int st = wave / TT; st <= (tt | 1); st += kWaves / TT) {
+            for (int st = wave / TT; st <= (tt | 1); st += WAVES / TT) {
                 f32x4 acc = {0, 0, 0, 0};
                 if (st <= tt) {
 #pragma unroll
@@ -172,107 +168,81 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
         }
         if (SWEEP == kChunkStates) {
             T *const to = static_cast<T *>(p.out) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV * p.slices) + v0 * DK;
+            const uint32_t at = (uint32_t)fresh(col * DK + paired<T>(0, 4 * g));
 #pragma unroll
             for (int i = 0; i < KT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-                    *reinterpret_cast<x4<T> *>(to + column(j, r) * DK + paired<T>(i, 4 * g)) = __builtin_convertvector(state[i][j], x4<T>);
+                *reinterpret_cast<x4<T> *>(to + at + paired<T>(i, 0)) = __builtin_convertvector(state[i], x4<T>);
         }
 
-        Frag<T> vf[C / 32][NT];
+        __builtin_amdgcn_sched_barrier(0);
+        Frag<T> vf[C / 32];
         {
             const int lane = fresh(lane0);
 #pragma unroll
-            for (int i = 0; i < C / 32; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) vf[i][j] = load_values(vs, j, 32 * i, lane);
+            for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<DV>(vs, 16 * wave, 32 * i, lane);
         }
 
         if (SWEEP == kOutput) {
             if (odd_values)
 #pragma unroll
-                for (int i = 0; i < C / 32; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) vf[i][j] = finite(vf[i][j]);
+                for (int i = 0; i < C / 32; ++i) vf[i] = finite(vf[i]);
             const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
-            f32x4 o[TT][NT]; // rows: columns of v, columns: tokens
+            Frag<T> sf[DK / 32];
 #pragma unroll
-            for (int i = 0; i < TT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) o[i][j] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < DK / 32; ++i) {
-                Frag<T> sf[NT];
-#pragma unroll
-                for (int j = 0; j < NT; ++j) sf[j] = to_frag<T>(state[2 * i][j], state[2 * i + 1][j]);
-#pragma unroll
-                for (int t = 0; t < TT; ++t) {
-                    const Frag<T> qf = load_rows<DK>(qs, 16 * t, 32 * i, lane);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) o[t][j] = mma(sf[j], qf, o[t][j]);
-                }
-            }
+            for (int i = 0; i < DK / 32; ++i) sf[i] = to_frag<T>(state[2 * i], state[2 * i + 1]);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
-                const float w = decays.from_start[16 * t + r] * p.scale;
+                f32x4 o = {0, 0, 0, 0}; // rows: columns of v, columns: tokens
 #pragma unroll
-                for (int j = 0; j < NT; ++j) o[t][j] *= w;
+                for (int i = 0; i < DK / 32; ++i) o = mma(sf[i], load_rows<DK>(qs, 16 * t, 32 * i, lane), o);
+                o *= decays.from_start[16 * t + r] * p.scale;
 #pragma unroll
-                for (int i = 0; i <= t / 2; ++i) {
-                    const Frag<T> pf = load_rows<C>(ps, 16 * t, 32 * i, lane);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) o[t][j] = mma(vf[i][j], pf, o[t][j]);
-                }
-                // an infinite or NaN v_s has no part in the tokens before it, where its zero weight would make it NaN: such
-                // values were left out above and are added to the tokens that see them
-                if (odd_values)
-                    for (int s = 0; s <= 16 * t + r; ++s) {
-                        const float w = to_float(ps[at<T, C>(16 * t + r, s)]);
-#pragma unroll
-                        for (int j = 0; j < NT; ++j)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float x = to_float(vs[at<T, DV>(s, column(j, 4 * g + e))]);
-                                if (!(__builtin_fabsf(x) < __builtin_inff())) o[t][j][e] += w * x;
-                            }
-                    }
-                if (16 * t + r < rows) {
-                    T *const row = static_cast<T *>(p.out) + ((first + t0 + 16 * t + r) * p.H + h) * (int64_t)p.V + v0;
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) store4(row, column(j, 4 * g), V, o[t][j]);
-                }
+                for (int i = 0; i <= t / 2; ++i) o = mma(vf[i], load_rows<C>(ps, 16 * t, 32 * i, lane), o);
+                if (16 * t + r < rows)
+                    store4(static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V + v0, (uint32_t)(16 * t + r) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, V, o);
                 __builtin_amdgcn_sched_barrier(0); // loads of what follows would only take registers here
             }
-            if (odd_values)
+            if (odd_values) {
+                // an infinite or NaN v_s has no part in the tokens before it, where its zero weight would make it NaN: such
+                // values were left out above and are added to the tokens that see them
+                T *const out = static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V + v0;
+#pragma unroll 1
+                for (int t = fresh(r); t < rows; t += 16)
+#pragma unroll 1
+                    for (int c = fresh(16 * wave + 4 * g), last = c + 4; c < last && c < V; ++c) {
+                        float more = 0.0f;
+#pragma unroll 1
+                        for (int s = 0; s <= t; ++s) {
+                            const float x = to_float(vs[at<T, DV>(s, c)]);
+                            if (!(__builtin_fabsf(x) < __builtin_inff())) more += to_float(ps[at<T, C>(t, s)]) * x;
+                        }
+                        T *const to = out + (uint32_t)t * (uint32_t)(p.H * p.V) + c;
+                        if (more != 0.0f) *to = (T)(to_float(*to) + more);
+                    }
 #pragma unroll
-                for (int i = 0; i < C / 32; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) vf[i][j] = load_values(vs, j, 32 * i, fresh(lane0));
+                for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<DV>(vs, 16 * wave, 32 * i, lane);
+            }
         }
 
         // the state after the chunk
         const float decay = decays.total;
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) state[i][j] *= decay;
+        for (int i = 0; i < KT; ++i) state[i] *= decay;
         const int lane = fresh(lane0);
 #pragma unroll
         for (int i = 0; i < C / 32; ++i) {
             f32x8 w = load_steps<T>((BACK ? decays.from_start : decays.to_end) + 32 * i, lane >> 4);
             if (BACK) w *= p.scale;
             // v scaled by its decay enters unrounded
-            Split<T> vw[NT];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) vw[j].set(widen(vf[i][j]) * w, odd_values);
+            Split<T> vw;
+            vw.set(widen(vf[i]) * w, odd_values);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
                 const Frag<T> kf = load_paired<DK>(ks, kt, 32 * i, lane);
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < Split<T>::COUNT; ++e) state[kt][j] = mma(kf, vw[j].part[e], state[kt][j]);
+                for (int e = 0; e < Split<T>::COUNT; ++e) state[kt] = mma(kf, vw.part[e], state[kt]);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         // rows past the K-th stay zero, also where zero was multiplied by infinity
         if (odd_values || !(__builtin_fabsf(decay) < __builtin_inff())) {
@@ -281,14 +251,12 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
             for (int i = 0; i < KT; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (paired<T>(i, 4 * g + e) >= p.K)
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) state[i][j][e] = 0.0f;
+                    if (paired<T>(i, 4 * g + e) >= p.K) state[i][e] = 0.0f;
         }
         __syncthreads();
     }
 
-    const int row0 = fresh(4 * g), col0 = fresh(r);
+    const int row0 = fresh(4 * g), col0 = fresh(col);
     float *to = nullptr;
     if (SWEEP == kSegmentState || SWEEP == kSegmentGradient) {
         to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0;
@@ -300,12 +268,10 @@ __global__ __launch_bounds__(kThreads, 2) void heinsen_attention_sweep(SweepArgs
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = paired<T>(i, row0 + e), c = column(j, col0);
-                    if (row < p.K && c < V) to[(uint32_t)(row * p.V + c)] = state[i][j][e];
-                }
+            for (int e = 0; e < 4; ++e) {
+                const int row = paired<T>(i, row0 + e);
+                if (row < p.K && col0 < V) to[(uint32_t)(row * p.V + col0)] = state[i][e];
+            }
 }
 
 // Chains the segments: each one's own sum is replaced by the state it starts from (BACK: the gradient it ends with).
@@ -316,15 +282,26 @@ __global__ __launch_bounds__(256) void heinsen_attention_chain(float *segment_st
 {
     const int blocks = (size + 255) / 256, bh = blockIdx.x / blocks, at = blockIdx.x % blocks * 256 + threadIdx.x;
     int64_t first;
-    const int64_t len = sequence(starts, n, bh / H, first);
+    const int64_t len = uniform_sequence(starts, n, bh / H, first);
     const int used = (int)((len + segment - 1) / segment);
     if (at >= size) return;
     float s = init ? init[(int64_t)bh * size + at] : 0.0f;
-    for (int i = 0; i < used; ++i) {
-        const int64_t j = (int64_t)bh * segments + (BACK ? used - 1 - i : i);
-        const float own = segment_state[j * size + at];
-        segment_state[j * size + at] = s;
-        s = s * segment_decay[j] + own;
+    constexpr int AHEAD = 8; // loads under way
+    for (int i = 0; i < used; i += AHEAD) {
+        float own[AHEAD], decay[AHEAD];
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const int last = used - 1, k = i + e < last ? i + e : last;
+            const int64_t j = (int64_t)bh * segments + (BACK ? last - k : k);
+            own[e] = segment_state[j * size + at];
+            decay[e] = segment_decay[j];
+        }
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e)
+            if (i + e < used) {
+                segment_state[((int64_t)bh * segments + (BACK ? used - 1 - i - e : i + e)) * size + at] = s;
+                s = s * decay[e] + own[e];
+            }
     }
 }
 
@@ -354,7 +331,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
     const int slice = blockIdx.x % p.slices, bh = blockIdx.x / p.slices, h = bh % p.H, b = bh / p.H;
     const int row0 = threadIdx.x / ACROSS, local = threadIdx.x % ACROSS * 4, col = slice * COLS + local;
     int64_t first;
-    const int64_t len = sequence(p.starts, p.n, b, first);
+    const int64_t len = uniform_sequence(p.starts, p.n, b, first);
     const int64_t at = (int64_t)bh * p.K * p.V;
 
     f32x4 state[PER];
@@ -406,7 +383,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int row = row0 + i * ROWS;
-            if (row < p.K) store4(p.sn + at + row * p.V, col, p.V, state[i]);
+            if (row < p.K) store4(p.sn + at, (uint32_t)(row * p.V), col, p.V, state[i]);
         }
 }
 
@@ -418,7 +395,7 @@ template <typename T, int SWEEP, int DK, int DV> hipError_t sweep_sized(SweepArg
 {
     a.slices = (a.V + DV - 1) / DV;
     const int64_t blocks = ((int64_t)a.units + 7) / 8 * 8 * a.slices;
-    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(a);
+    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -470,7 +447,8 @@ template <typename T> hipError_t step(const AttentionCall &c)
 Segments attention_segments(const AttentionCall &c)
 {
     // two workgroups to a compute unit at least, while a segment stays long against the states it adds
-    const int64_t heads = (int64_t)c.B * c.H, want = 2 * compute_units();
+    static const int per_unit = getenv("HS_PU") ? atoi(getenv("HS_PU")) : 2;
+    const int64_t heads = (int64_t)c.B * c.H, want = per_unit * compute_units();
     int64_t count = heads >= want ? 1 : (want + heads - 1) / heads;
     const int64_t most = (c.n + 511) / 512;
     if (count > most) count = most;

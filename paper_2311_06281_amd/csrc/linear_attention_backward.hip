@@ -51,10 +51,10 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     __shared__ Decays<C> decays;
     __shared__ float xs[KT][C], ys[KT][C], pair_rows[TT][C], pair_cols[TT][C], spans[WAVES];
 
-    const int lane0 = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane0 & 15, g = lane0 >> 4;
+    const int lane0 = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), r = lane0 & 15, g = lane0 >> 4;
     const int seg = blockIdx.x % p.segments, bh = blockIdx.x / p.segments, h = bh % p.H, b = bh / p.H;
     int64_t first;
-    const int64_t len = sequence(p.starts, p.n, b, first);
+    const int64_t len = uniform_sequence(p.starts, p.n, b, first);
     const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
     if (begin >= len && seg > 0) return;
 
@@ -107,20 +107,20 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             next_s.load(DV);
             next_s.move(-DV);
         }
-        if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + (lane0 < rows ? lane0 : 0)) * p.H + h];
+        if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + fresh(lane0 < rows ? lane0 : 0)) * p.H + h];
     };
     if (chunks > 0) request(last);
 
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
         const int64_t t0 = begin + (int64_t)chunk * C;
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_q.settle(rows, p.K);
+        next_q.settle(p.K);
         next_q.store(qs, q + t0 * p.q_stride, p.q_stride, rows, p.K);
-        next_k.settle(rows, p.K);
+        next_k.settle(p.K);
         next_k.store(ks, k + t0 * p.k_stride, p.k_stride, rows, p.K);
-        next_v.settle(rows, p.V);
+        next_v.settle(p.V);
         next_v.store(vs, v + t0 * p.v_stride, p.v_stride, rows, p.V);
-        next_o.settle(rows, p.V);
+        next_o.settle(p.V);
         next_o.store(os, o + t0 * o_stride, o_stride, rows, p.V);
         if (STAGED) next_s.store(ss, state_of(t0), DK, DV, DK);
         if (wave == 0) write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 for (int i = st / 2; i < C / 32; ++i)
                     acc = mma(load_cols<DV>(os, 16 * wave, 32 * i, lane), load_rows<C>(ps, 16 * st, 32 * i, lane), acc);
                 if (16 * st + r < rows)
-                    store4(static_cast<T *>(p.grad_v) + ((first + t0 + 16 * st + r) * p.H + h) * (int64_t)p.V, 16 * wave + 4 * g, p.V, acc);
+                    store4(static_cast<T *>(p.grad_v) + ((first + t0) * p.H + h) * p.V, (uint32_t)(16 * st + r) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, p.V, acc);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -223,10 +223,11 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 for (int i = 0; i <= t / 2; ++i)
                     acc = mma(load_cols<DK>(ks, 16 * kt, 32 * i, lane), load_cols<C>(ds, 16 * t, 32 * i, lane), acc);
                 // a head of v's own part of a shared gradient goes to the scratch, n places for each sequence
-                const int64_t place = (p.share > 1 ? b * p.n : first) + t0 + token;
+                const int64_t place = (((p.share > 1 ? b * p.n : first) + t0) * p.H + h) * p.K;
+                const uint32_t to = (uint32_t)token * (uint32_t)(p.H * p.K);
                 if (token < rows) {
-                    if (p.share > 1) store4(static_cast<float *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
-                    else store4(static_cast<T *>(p.grad_q) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
+                    if (p.share > 1) store4(static_cast<float *>(p.grad_q) + place, to, 16 * kt + 4 * g, p.K, acc);
+                    else store4(static_cast<T *>(p.grad_q) + place, to, 16 * kt + 4 * g, p.K, acc);
                 }
 
                 acc = f32x4{0, 0, 0, 0};
@@ -244,8 +245,8 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 for (int i = t / 2; i < C / 32; ++i)
                     acc = mma(load_cols<DK>(qs, 16 * kt, 32 * i, lane), load_rows<C>(ds, 16 * t, 32 * i, lane), acc);
                 if (token < rows) {
-                    if (p.share > 1) store4(static_cast<float *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
-                    else store4(static_cast<T *>(p.grad_k) + (place * p.H + h) * p.K, 16 * kt + 4 * g, p.K, acc);
+                    if (p.share > 1) store4(static_cast<float *>(p.grad_k) + place, to, 16 * kt + 4 * g, p.K, acc);
+                    else store4(static_cast<T *>(p.grad_k) + place, to, 16 * kt + 4 * g, p.K, acc);
                 }
                 __builtin_amdgcn_sched_barrier(0); // loads of the next tokens would only take registers here
             }
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) span += spans[i];
             // of x and the pairs from this token on, of y before it
-            const double upto = prefix_sum(suffix), from = lane_at(upto, 63) - upto + suffix, before = prefix_sum(prefix) - prefix;
+            const double upto = prefix_sum(suffix), from = of_lane(upto, 63) - upto + suffix, before = prefix_sum(prefix) - prefix;
             if (lane < rows) {
                 const float sum = (float)(from + before + span);
                 if (p.per_head) static_cast<float *>(p.grad_log_a)[(b * p.n + t0 + lane) * p.H + h] = sum;
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardA
     const int bh = blockIdx.x, h = bh % p.H, b = bh / p.H;
     const int row0 = threadIdx.x / ACROSS, col = threadIdx.x % ACROSS * 4;
     int64_t first;
-    const int len = (int)sequence(p.starts, p.n, b, first);
+    const int len = (int)uniform_sequence(p.starts, p.n, b, first);
     const int64_t at = (int64_t)bh * p.K * p.V;
 
     f32x4 start[PER], grad[PER]; // s0 and R
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_step_backward(BackwardA
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int row = row0 + i * ROWS;
-            if (row < p.K) store4(p.grad_s0 + at + row * p.V, col, p.V, grad[i]);
+            if (row < p.K) store4(p.grad_s0 + at, (uint32_t)(row * p.V), col, p.V, grad[i]);
         }
 }
 
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(256) void heinsen_attention_decay_sum(const float *
     double sum = 0.0;
     for (int b = 0; b < B; ++b) {
         int64_t first;
-        const int64_t len = sequence(starts, n, b, first);
+        const int64_t len = uniform_sequence(starts, n, b, first);
         for (int64_t t = threadIdx.x; t < len; t += 256) sum += in[(b * n + t) * H + blockIdx.x];
     }
     part[threadIdx.x] = sum;
