@@ -18,6 +18,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T> struct Vec;
@@ -54,28 +55,39 @@ template <typename T> __device__ static inline int paired(int tile, int r)
     return sizeof(T) == 2 ? 32 * (tile >> 1) + 8 * (r >> 2) + 4 * (tile & 1) + (r & 3) : 16 * tile + r;
 }
 
-// Tiles of rows of D entries in LDS.  The 16-byte pieces of a row change places with the row's number, so that the accesses
-// below, sixteen lanes at a time, each touch all banks once: a piece of sixteen rows, four neighbouring or every second piece
-// of four rows (bfloat16), four neighbouring pieces of every fourth row (float32).
-template <typename T, int D> __device__ static inline int at(int row, int col)
-{
-    constexpr int N = 16 / (int)sizeof(T), PIECES = D / N;
+// Tiles of rows of D entries in LDS: where entry (row, col) is.
+//
+// Padded: rows a few banks apart, so that sixteen lanes that read a 16-byte piece of a row each touch all banks once, and those
+// that read pieces of four rows twice at most.  Addresses are a lane's own plus a constant.
+// Swapped: no padding; the pieces of a row change places with the row's number, so that the accesses below each touch all
+// banks once.  Addresses take a few instructions: for the kernel that fills LDS.
+template <typename T_, int D_> struct Padded {
+    typedef T_ T;
+    static constexpr int D = D_, PITCH = D + (sizeof(T) == 2 ? 24 : 4);
+    __device__ static int at(int row, int col) { return row * PITCH + col; }
+};
+template <typename T_, int D_> struct Swapped {
+    typedef T_ T;
+    static constexpr int D = D_, PITCH = D, N = 16 / (int)sizeof(T), PIECES = D / N;
     static_assert(PIECES >= 8, "eight pieces to a row at least");
-    int swap;
-    if (PIECES >= 16) swap = sizeof(T) == 2 ? ((row & 3) << 2) | ((row >> 2) & 3) : row & 15;
-    else swap = sizeof(T) == 2 ? ((row & 2) << 1) | ((row >> 2) & 3) : (row >> 1) & 7;
-    return row * D + (((col / N) ^ swap) * N) + col % N;
-}
+    __device__ static int at(int row, int col)
+    {
+        int swap;
+        if (PIECES >= 16) swap = sizeof(T) == 2 ? ((row & 3) << 2) | ((row >> 2) & 3) : row & 15;
+        else swap = sizeof(T) == 2 ? ((row & 2) << 1) | ((row >> 2) & 3) : (row >> 1) & 7;
+        return row * D + (((col / N) ^ swap) * N) + col % N;
+    }
+};
 
 // Fragment of rows row0.. of a tile, contraction along the row from k0 on.
-template <int D> __device__ static inline bf16x8 load_rows(const __bf16 *tile, int row0, int k0, int lane)
+template <typename L> __device__ static inline bf16x8 load_rows(const __bf16 *tile, int row0, int k0, int lane)
 {
-    return *reinterpret_cast<const bf16x8 *>(tile + at<__bf16, D>(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
+    return *reinterpret_cast<const bf16x8 *>(tile + L::at(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
 }
-template <int D> __device__ static inline f32x8 load_rows(const float *tile, int row0, int k0, int lane)
+template <typename L> __device__ static inline f32x8 load_rows(const float *tile, int row0, int k0, int lane)
 {
     const int row = row0 + (lane & 15), col = k0 + 4 * (lane >> 4);
-    return join<float>(*reinterpret_cast<const f32x4 *>(tile + at<float, D>(row, col)), *reinterpret_cast<const f32x4 *>(tile + at<float, D>(row, col + 16)));
+    return join<float>(*reinterpret_cast<const f32x4 *>(tile + L::at(row, col)), *reinterpret_cast<const f32x4 *>(tile + L::at(row, col + 16)));
 }
 
 // Fragment of columns of a tile, contraction down the rows from k0 on.
@@ -85,26 +97,26 @@ __device__ static inline bf16x4 transposed4(const __bf16 *p)
                                           (__attribute__((address_space(3))) i16x4 *)(const_cast<__bf16 *>(p))));
 }
 // sixteen lanes read four entries each of four rows, `apart` entries from one lane's to the next one's, and get a column each
-template <int D> __device__ static inline bf16x8 columns(const __bf16 *tile, int col0, int apart, int k0, int lane)
+template <typename L> __device__ static inline bf16x8 columns(const __bf16 *tile, int col0, int apart, int k0, int lane)
 {
     const int row = k0 + 8 * (lane >> 4) + ((lane & 15) >> 2), col = col0 + apart * (lane & 3);
-    return join<__bf16>(transposed4(tile + at<__bf16, D>(row, col)), transposed4(tile + at<__bf16, D>(row + 4, col)));
+    return join<__bf16>(transposed4(tile + L::at(row, col)), transposed4(tile + L::at(row + 4, col)));
 }
-template <int D> __device__ static inline f32x8 columns(const float *tile, int col0, int, int k0, int lane)
+template <typename L> __device__ static inline f32x8 columns(const float *tile, int col0, int, int k0, int lane)
 {
     f32x8 f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = tile[at<float, D>(k0 + step_of<float>(lane >> 4, e), col0 + (lane & 15))];
+    for (int e = 0; e < 8; ++e) f[e] = tile[L::at(k0 + step_of<float>(lane >> 4, e), col0 + (lane & 15))];
     return f;
 }
 // columns 16 * tile.., or those that the rows of block `tile` of a state stand for
-template <int D, typename T> __device__ static inline Frag<T> load_cols(const T *tile, int col0, int k0, int lane)
+template <typename L, typename T> __device__ static inline Frag<T> load_cols(const T *tile, int col0, int k0, int lane)
 {
-    return columns<D>(tile, col0, 4, k0, lane);
+    return columns<L>(tile, col0, 4, k0, lane);
 }
-template <int D, typename T> __device__ static inline Frag<T> load_paired(const T *tile, int block, int k0, int lane)
+template <typename L, typename T> __device__ static inline Frag<T> load_paired(const T *tile, int block, int k0, int lane)
 {
-    return columns<D>(tile, paired<T>(block, 0), sizeof(T) == 2 ? 8 : 4, k0, lane);
+    return columns<L>(tile, paired<T>(block, 0), sizeof(T) == 2 ? 8 : 4, k0, lane);
 }
 
 // Eight float32 in the fragment's order of steps, from k0 on.
@@ -188,15 +200,17 @@ template <> struct Unaligned<__bf16> {
 #define AS_GLOBAL __attribute__((address_space(1)))
 
 // A tile of C rows of D entries on its way from global memory to LDS, in registers.
-template <typename T, int C, int D, int THREADS> struct TileLoad {
-    static constexpr int N = 16 / (int)sizeof(T);
+// NARROW: rows may be shorter than a vector.
+template <typename L, int C, int THREADS, bool NARROW> struct TileLoad {
+    typedef typename L::T T;
+    static constexpr int D = L::D, N = 16 / (int)sizeof(T);
     static constexpr int PER_ROW = D / N;
     static constexpr int AT_ONCE = THREADS / PER_ROW; // rows
     static constexpr int COUNT = C / AT_ONCE;
     static_assert(C % AT_ONCE == 0 && THREADS % PER_ROW == 0, "whole rounds of whole rows");
     u32x4 v[COUNT];
     uint64_t next;      // address of the next tile's first row
-    uint32_t step, end; // bytes from row to row, and of a row (none: too short for a vector)
+    uint32_t step, end; // bytes from row to row, and of a row (none: shorter than a vector)
 
     __device__ static int col() { return threadIdx.x % PER_ROW * N; }
     __device__ static int row(int i) { return threadIdx.x / PER_ROW + i * AT_ONCE; }
@@ -207,7 +221,7 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
     {
         next = uniform((uint64_t)reinterpret_cast<uintptr_t>(base));
         step = uniform((uint32_t)stride * (uint32_t)sizeof(T));
-        end = d < N ? 0 : (uint32_t)d * (uint32_t)sizeof(T);
+        end = NARROW && d < N ? 0 : (uint32_t)d * (uint32_t)sizeof(T);
     }
     // Rows past the last are zero: the hardware reads nothing past the end that it is told.
     __device__ void load(int rows)
@@ -215,7 +229,7 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
         const uint32_t thread = (uint32_t)fresh((int)threadIdx.x), piece = thread % PER_ROW * 16, last = end - 16;
         const uint32_t offset = thread / PER_ROW * step + (piece < last ? piece : last);
         const __amdgpu_buffer_rsrc_t memory =
-            __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(next), 0, end == 0 ? 0 : (int)((uint32_t)(rows - 1) * step + end), 0x00020000);
+            __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(next), 0, NARROW && end == 0 ? 0 : (int)((uint32_t)(rows - 1) * step + end), 0x00020000);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(memory, (int)offset, (int)(step * (i * AT_ONCE)), 0));
     }
@@ -223,7 +237,7 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
     // Puts what was read of a row's last piece in place: entries from the d-th on are zero.
     __device__ void settle(int d)
     {
-        if (d < D && d >= N) {
+        if (d < D && !(NARROW && d < N)) {
             const int col = fresh(this->col()), shift = (col - (col < d - N ? col : d - N)) * 8 * (int)sizeof(T);
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
@@ -240,15 +254,15 @@ template <typename T, int C, int D, int THREADS> struct TileLoad {
     __device__ bool store(T *tile, const T *base, int64_t stride, int rows, int d) const
     {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) *reinterpret_cast<u32x4 *>(tile + at<T, D>(row(i), col())) = v[i];
+        for (int i = 0; i < COUNT; ++i) *reinterpret_cast<u32x4 *>(tile + L::at(row(i), col())) = v[i];
         bool odd = false;
-        if (d < N && col() == 0) {
+        if (NARROW && d < N && col() == 0) {
 #pragma unroll 1
             for (int at_row = fresh(row(0)); at_row < rows; at_row += THREADS / PER_ROW)
 #pragma unroll 1
                 for (int j = 0; j < d; ++j) {
                     const T x = base[at_row * stride + j];
-                    tile[at<T, D>(at_row, j)] = x;
+                    tile[L::at(at_row, j)] = x;
                     odd |= !(__builtin_fabsf((float)x) < __builtin_inff());
                 }
         }
@@ -292,6 +306,16 @@ template <typename T> __device__ static inline void store4(T *base, uint32_t row
 #pragma unroll
         for (int i = 0; i < 3; ++i)
             if (col + i < d) *(T AS_GLOBAL *)(to + offset + i * (uint32_t)sizeof(T)) = e[i];
+}
+
+// four entries `offset` + `more` bytes behind the start of `memory`
+__device__ static inline void buffer_store(bf16x4 e, __amdgpu_buffer_rsrc_t memory, uint32_t offset, uint32_t more)
+{
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, e), memory, (int)offset, (int)more, 0);
+}
+__device__ static inline void buffer_store(f32x4 e, __amdgpu_buffer_rsrc_t memory, uint32_t offset, uint32_t more)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, e), memory, (int)offset, (int)more, 0);
 }
 
 // ---- decays within a chunk ------------------------------------------------------------------------------------

@@ -49,15 +49,18 @@ __device__ static inline int unit_and_slice(int slices, int &slice)
 // A workgroup takes one segment of one head's tokens and goes through its chunks, DV columns of the state in registers, sixteen
 // to a wave.  kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
 // (k, v) and gives the segment's own part of the gradient of the state it starts from.
-template <typename T, int C, int DK, int DV, int SWEEP>
+template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW>
 __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p)
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
     constexpr bool BACK = SWEEP == kSegmentGradient;
-    __shared__ __align__(16) T ks[C * DK];
-    __shared__ __align__(16) T vs[C * DV];
-    __shared__ __align__(16) T qs[SWEEP == kOutput ? C * DK : 16];
-    __shared__ __align__(16) T ps[SWEEP == kOutput ? C * C : 16];
+    typedef Padded<T, DK> LK;
+    typedef Padded<T, DV> LV;
+    typedef Padded<T, C> LC;
+    __shared__ __align__(16) T ks[C * LK::PITCH];
+    __shared__ __align__(16) T vs[C * LV::PITCH];
+    __shared__ __align__(16) T qs[SWEEP == kOutput ? C * LK::PITCH : 16];
+    __shared__ __align__(16) T ps[SWEEP == kOutput ? C * LC::PITCH : 16];
     __shared__ Decays<C> decays;
     __shared__ int not_finite[2]; // of even and odd chunks
 
@@ -97,8 +100,8 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
 
     const int chunks = (int)((end - begin + C - 1) / C);
     auto chunk_start = [&](int i) { return begin + (int64_t)(BACK ? chunks - 1 - i : i) * C; };
-    TileLoad<T, C, DK, THREADS> next_q, next_k;
-    TileLoad<T, C, DV, THREADS> next_v;
+    TileLoad<LK, C, THREADS, NARROW> next_q, next_k;
+    TileLoad<LV, C, THREADS, NARROW> next_v;
     T next_log_a = (T)0.0f;
     next_k.start(k + chunk_start(0) * p.k_stride, p.k_stride, p.K);
     next_v.start(v + chunk_start(0) * p.v_stride, p.v_stride, V);
@@ -144,16 +147,16 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
             // the weights of the chunk's tokens for one another, scale e^{G_t-G_s} q_t . k_s, in tiles of 16 x 16: this wave's
             // are those of tokens t in one row of tiles
             const int tt = wave % TT;
-            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
+            const int lane = lane0;
             Frag<T> qf[DK / 32];
 #pragma unroll
-            for (int i = 0; i < DK / 32; ++i) qf[i] = load_rows<DK>(qs, 16 * tt, 32 * i, lane);
+            for (int i = 0; i < DK / 32; ++i) qf[i] = load_rows<LK>(qs, 16 * tt, 32 * i, lane);
             const float whole_t = decays.whole[16 * tt + r], part_t = decays.part[16 * tt + r];
             for (int st = wave / TT; st <= (tt | 1); st += WAVES / TT) {
                 f32x4 acc = {0, 0, 0, 0};
                 if (st <= tt) {
 #pragma unroll
-                    for (int i = 0; i < DK / 32; ++i) acc = mma(load_rows<DK>(ks, 16 * st, 32 * i, lane), qf[i], acc);
+                    for (int i = 0; i < DK / 32; ++i) acc = mma(load_rows<LK>(ks, 16 * st, 32 * i, lane), qf[i], acc);
                     const f32x4 whole = *reinterpret_cast<const f32x4 *>(&decays.whole[16 * st + 4 * g]);
                     const f32x4 part = *reinterpret_cast<const f32x4 *>(&decays.part[16 * st + 4 * g]);
 #pragma unroll
@@ -162,7 +165,7 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
                         acc[e] = 16 * st + 4 * g + e <= 16 * tt + r ? acc[e] * w : 0.0f;
                     }
                 }
-                *reinterpret_cast<x4<T> *>(ps + at<T, C>(16 * tt + r, 16 * st + 4 * g)) = __builtin_convertvector(acc, x4<T>);
+                *reinterpret_cast<x4<T> *>(ps + LC::at(16 * tt + r, 16 * st + 4 * g)) = __builtin_convertvector(acc, x4<T>);
             }
             __syncthreads();
         }
@@ -177,16 +180,21 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
         __builtin_amdgcn_sched_barrier(0);
         Frag<T> vf[C / 32];
         {
-            const int lane = fresh(lane0);
+            const int lane = lane0;
 #pragma unroll
-            for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<DV>(vs, 16 * wave, 32 * i, lane);
+            for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<LV>(vs, 16 * wave, 32 * i, lane);
         }
 
         if (SWEEP == kOutput) {
             if (odd_values)
 #pragma unroll
                 for (int i = 0; i < C / 32; ++i) vf[i] = finite(vf[i]);
-            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
+            const int lane = lane0;
+            T *const out_base = static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V + v0;
+            const uint32_t out_step = (uint32_t)(p.H * p.V) * (uint32_t)sizeof(T), out_offset = r * out_step + (16 * wave + 4 * g) * (uint32_t)sizeof(T);
+            const __amdgpu_buffer_rsrc_t out =
+                __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(uniform((uint64_t)reinterpret_cast<uintptr_t>(out_base))), 0,
+                                                  (int)((uint32_t)(rows - 1) * out_step + DV * (uint32_t)sizeof(T)), 0x00020000);
             Frag<T> sf[DK / 32];
 #pragma unroll
             for (int i = 0; i < DK / 32; ++i) sf[i] = to_frag<T>(state[2 * i], state[2 * i + 1]);
@@ -194,12 +202,15 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
             for (int t = 0; t < TT; ++t) {
                 f32x4 o = {0, 0, 0, 0}; // rows: columns of v, columns: tokens
 #pragma unroll
-                for (int i = 0; i < DK / 32; ++i) o = mma(sf[i], load_rows<DK>(qs, 16 * t, 32 * i, lane), o);
+                for (int i = 0; i < DK / 32; ++i) o = mma(sf[i], load_rows<LK>(qs, 16 * t, 32 * i, lane), o);
                 o *= decays.from_start[16 * t + r] * p.scale;
 #pragma unroll
-                for (int i = 0; i <= t / 2; ++i) o = mma(vf[i], load_rows<C>(ps, 16 * t, 32 * i, lane), o);
-                if (16 * t + r < rows)
-                    store4(static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V + v0, (uint32_t)(16 * t + r) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, V, o);
+                for (int i = 0; i <= t / 2; ++i) o = mma(vf[i], load_rows<LC>(ps, 16 * t, 32 * i, lane), o);
+                if (V == DV) { // tokens past the last are not written: the hardware writes nothing past the end that it is told
+                    buffer_store(__builtin_convertvector(o, x4<T>), out, out_offset, out_step * (16 * t));
+                } else if (16 * t + r < rows) {
+                    store4(out_base, (uint32_t)(16 * t + fresh(r)) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, V, o);
+                }
                 __builtin_amdgcn_sched_barrier(0); // loads of what follows would only take registers here
             }
             if (odd_values) {
@@ -213,14 +224,14 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
                         float more = 0.0f;
 #pragma unroll 1
                         for (int s = 0; s <= t; ++s) {
-                            const float x = to_float(vs[at<T, DV>(s, c)]);
-                            if (!(__builtin_fabsf(x) < __builtin_inff())) more += to_float(ps[at<T, C>(t, s)]) * x;
+                            const float x = to_float(vs[LV::at(s, c)]);
+                            if (!(__builtin_fabsf(x) < __builtin_inff())) more += to_float(ps[LC::at(t, s)]) * x;
                         }
                         T *const to = out + (uint32_t)t * (uint32_t)(p.H * p.V) + c;
                         if (more != 0.0f) *to = (T)(to_float(*to) + more);
                     }
 #pragma unroll
-                for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<DV>(vs, 16 * wave, 32 * i, lane);
+                for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<LV>(vs, 16 * wave, 32 * i, lane);
             }
         }
 
@@ -228,7 +239,7 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
         const float decay = decays.total;
 #pragma unroll
         for (int i = 0; i < KT; ++i) state[i] *= decay;
-        const int lane = fresh(lane0);
+        const int lane = lane0;
 #pragma unroll
         for (int i = 0; i < C / 32; ++i) {
             f32x8 w = load_steps<T>((BACK ? decays.from_start : decays.to_end) + 32 * i, lane >> 4);
@@ -238,7 +249,7 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
             vw.set(widen(vf[i]) * w, odd_values);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                const Frag<T> kf = load_paired<DK>(ks, kt, 32 * i, lane);
+                const Frag<T> kf = load_paired<LK>(ks, kt, 32 * i, lane);
 #pragma unroll
                 for (int e = 0; e < Split<T>::COUNT; ++e) state[kt] = mma(kf, vw.part[e], state[kt]);
             }
@@ -391,18 +402,23 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 
 template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 : 32; }
 
-template <typename T, int SWEEP, int DK, int DV> hipError_t sweep_sized(SweepArgs &a, hipStream_t stream)
+template <typename T, int SWEEP, int DK, int DV, bool NARROW> hipError_t sweep_sized(SweepArgs &a, hipStream_t stream)
 {
     a.slices = (a.V + DV - 1) / DV;
     const int64_t blocks = ((int64_t)a.units + 7) / 8 * 8 * a.slices;
-    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
+    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP, NARROW><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <typename T, int SWEEP> hipError_t sweep(SweepArgs &a, hipStream_t stream)
 {
-    if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64>(a, stream) : sweep_sized<T, SWEEP, 64, 128>(a, stream);
-    return a.V <= 64 ? sweep_sized<T, SWEEP, 128, 64>(a, stream) : sweep_sized<T, SWEEP, 128, 128>(a, stream);
+    constexpr int N = 16 / (int)sizeof(T);
+    if (a.K < N || a.V < N) {
+        if (a.K > 64) return sweep_sized<T, SWEEP, 128, 64, true>(a, stream);
+        return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, true>(a, stream) : sweep_sized<T, SWEEP, 64, 128, true>(a, stream);
+    }
+    if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, false>(a, stream) : sweep_sized<T, SWEEP, 64, 128, false>(a, stream);
+    return a.V <= 64 ? sweep_sized<T, SWEEP, 128, 64, false>(a, stream) : sweep_sized<T, SWEEP, 128, 128, false>(a, stream);
 }
 
 SweepArgs sweep_args(const AttentionCall &c, const Segments &s)

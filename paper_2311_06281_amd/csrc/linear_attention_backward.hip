@@ -35,11 +35,14 @@ struct BackwardArgs {
 
 // A workgroup takes one segment of one head's tokens from its last chunk to its first; the gradient R of the state is in
 // registers, 16 columns to a wave.
-template <typename T, int C, int DK, int DV>
+template <typename T, int C, int DK, int DV, bool NARROW>
 __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(BackwardArgs p)
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
     constexpr bool STAGED = sizeof(T) == 2;        // the chunk's first state goes through LDS; in float32 there is no room
+    typedef Swapped<T, DK> LK;
+    typedef Swapped<T, DV> LV;
+    typedef Swapped<T, C> LC;
     __shared__ __align__(16) T qs[C * DK];
     __shared__ __align__(16) T ks[C * DK];
     __shared__ __align__(16) T vs[C * DV];
@@ -82,9 +85,9 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         }
 
     const int chunks = (int)((end - begin + C - 1) / C);
-    TileLoad<T, C, DK, THREADS> next_q, next_k;
-    TileLoad<T, C, DV, THREADS> next_v, next_o;
-    TileLoad<T, STAGED ? DV : THREADS * 16 / (int)sizeof(T) / DK, DK, THREADS> next_s;
+    TileLoad<LK, C, THREADS, NARROW> next_q, next_k;
+    TileLoad<LV, C, THREADS, NARROW> next_v, next_o;
+    TileLoad<LK, STAGED ? DV : THREADS * 16 / (int)sizeof(T) / DK, THREADS, false> next_s;
     T next_log_a = (T)0.0f;
     auto state_of = [&](int64_t t0) { return static_cast<const T *>(p.states) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV); };
     const int64_t last = begin + (int64_t)(chunks - 1) * C; // the last chunk's first token
@@ -126,7 +129,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         if (wave == 0) write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
 #pragma unroll
         for (int i = 0; i < KT; ++i)
-            *reinterpret_cast<x4<T> *>(rs + at<T, DK>(col, paired<T>(i, 4 * g))) = __builtin_convertvector(grad[i], x4<T>);
+            *reinterpret_cast<x4<T> *>(rs + LK::at(col, paired<T>(i, 4 * g))) = __builtin_convertvector(grad[i], x4<T>);
         __syncthreads();
         if (chunk > 0) request(t0 - C);
         const T *const state = state_of(t0);
@@ -140,9 +143,9 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             f32x4 pt = {0, 0, 0, 0}, dt = {0, 0, 0, 0};
             if (st <= tt) {
 #pragma unroll
-                for (int i = 0; i < DK / 32; ++i) pt = mma(load_rows<DK>(qs, 16 * tt, 32 * i, lane), load_rows<DK>(ks, 16 * st, 32 * i, lane), pt);
+                for (int i = 0; i < DK / 32; ++i) pt = mma(load_rows<LK>(qs, 16 * tt, 32 * i, lane), load_rows<LK>(ks, 16 * st, 32 * i, lane), pt);
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) dt = mma(load_rows<DV>(os, 16 * tt, 32 * i, lane), load_rows<DV>(vs, 16 * st, 32 * i, lane), dt);
+                for (int i = 0; i < DV / 32; ++i) dt = mma(load_rows<LV>(os, 16 * tt, 32 * i, lane), load_rows<LV>(vs, 16 * st, 32 * i, lane), dt);
                 const int s = 16 * st + r; // rows: tokens t, columns: tokens s
                 const float whole_s = decays.whole[s], part_s = decays.part[s];
                 float below = 0.0f;
@@ -166,8 +169,8 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                     for (int e = 0; e < 4; ++e) across[e] += __shfl_xor(across[e], by);
                 if (r == 0) *reinterpret_cast<f32x4 *>(&pair_rows[st][16 * tt + 4 * g]) = across;
             }
-            *reinterpret_cast<x4<T> *>(ps + at<T, C>(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(pt, x4<T>);
-            *reinterpret_cast<x4<T> *>(ds + at<T, C>(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(dt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ps + LC::at(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(pt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ds + LC::at(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(dt, x4<T>);
         }
         __syncthreads();
 
@@ -181,11 +184,11 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             for (int st = 0; st < TT; ++st) {
                 f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < DK / 32; ++i) acc = mma(rf[i], load_rows<DK>(ks, 16 * st, 32 * i, lane), acc);
+                for (int i = 0; i < DK / 32; ++i) acc = mma(rf[i], load_rows<LK>(ks, 16 * st, 32 * i, lane), acc);
                 acc *= decays.to_end[16 * st + r];
 #pragma unroll
                 for (int i = st / 2; i < C / 32; ++i)
-                    acc = mma(load_cols<DV>(os, 16 * wave, 32 * i, lane), load_rows<C>(ps, 16 * st, 32 * i, lane), acc);
+                    acc = mma(load_cols<LV>(os, 16 * wave, 32 * i, lane), load_rows<LC>(ps, 16 * st, 32 * i, lane), acc);
                 if (16 * st + r < rows)
                     store4(static_cast<T *>(p.grad_v) + ((first + t0) * p.H + h) * p.V, (uint32_t)(16 * st + r) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, p.V, acc);
                 __builtin_amdgcn_sched_barrier(0);
@@ -197,11 +200,11 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             Frag<T> sf[DV / 32], rf[DV / 32];
 #pragma unroll
             for (int i = 0; i < DV / 32; ++i) {
-                if (STAGED) sf[i] = load_cols<DK>(ss, 16 * kt, 32 * i, lane);
+                if (STAGED) sf[i] = load_cols<LK>(ss, 16 * kt, 32 * i, lane);
                 else
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sf[i][e] = state[(32 * i + step_of<T>(g, e)) * DK + 16 * kt + r];
-                rf[i] = load_cols<DK>(rs, 16 * kt, 32 * i, lane);
+                rf[i] = load_cols<LK>(rs, 16 * kt, 32 * i, lane);
             }
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
@@ -210,9 +213,9 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 const int token = 16 * t + r;
                 f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) acc = mma(sf[i], load_rows<DV>(os, 16 * t, 32 * i, lane), acc);
+                for (int i = 0; i < DV / 32; ++i) acc = mma(sf[i], load_rows<LV>(os, 16 * t, 32 * i, lane), acc);
                 acc *= decays.from_start[token] * p.scale;
-                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + at<T, DK>(token, 16 * kt + 4 * g));
+                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + LK::at(token, 16 * kt + 4 * g));
                 float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
@@ -221,7 +224,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 if (g == 0) xs[kt][token] = sum;
 #pragma unroll
                 for (int i = 0; i <= t / 2; ++i)
-                    acc = mma(load_cols<DK>(ks, 16 * kt, 32 * i, lane), load_cols<C>(ds, 16 * t, 32 * i, lane), acc);
+                    acc = mma(load_cols<LK>(ks, 16 * kt, 32 * i, lane), load_cols<LC>(ds, 16 * t, 32 * i, lane), acc);
                 // a head of v's own part of a shared gradient goes to the scratch, n places for each sequence
                 const int64_t place = (((p.share > 1 ? b * p.n : first) + t0) * p.H + h) * p.K;
                 const uint32_t to = (uint32_t)token * (uint32_t)(p.H * p.K);
@@ -232,9 +235,9 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 
                 acc = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) acc = mma(rf[i], load_rows<DV>(vs, 16 * t, 32 * i, lane), acc);
+                for (int i = 0; i < DV / 32; ++i) acc = mma(rf[i], load_rows<LV>(vs, 16 * t, 32 * i, lane), acc);
                 acc *= decays.to_end[token];
-                own = *reinterpret_cast<const x4<T> *>(ks + at<T, DK>(token, 16 * kt + 4 * g));
+                own = *reinterpret_cast<const x4<T> *>(ks + LK::at(token, 16 * kt + 4 * g));
                 sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 if (g == 0) ys[kt][token] = sum;
 #pragma unroll
                 for (int i = t / 2; i < C / 32; ++i)
-                    acc = mma(load_cols<DK>(qs, 16 * kt, 32 * i, lane), load_rows<C>(ds, 16 * t, 32 * i, lane), acc);
+                    acc = mma(load_cols<LK>(qs, 16 * kt, 32 * i, lane), load_rows<LC>(ds, 16 * t, 32 * i, lane), acc);
                 if (token < rows) {
                     if (p.share > 1) store4(static_cast<float *>(p.grad_k) + place, to, 16 * kt + 4 * g, p.K, acc);
                     else store4(static_cast<T *>(p.grad_k) + place, to, 16 * kt + 4 * g, p.K, acc);
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < KT; ++i) {
-                const x4<T> s = STAGED ? *reinterpret_cast<const x4<T> *>(ss + at<T, DK>(col, paired<T>(i, 4 * g)))
+                const x4<T> s = STAGED ? *reinterpret_cast<const x4<T> *>(ss + LK::at(col, paired<T>(i, 4 * g)))
                                        : *reinterpret_cast<const x4<T> *>(state + col * DK + paired<T>(i, 4 * g));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += grad[i][e] * to_float(s[e]);
@@ -269,13 +272,13 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
             for (int i = 0; i < C / 32; ++i) {
                 const int lane = fresh(lane0), g = lane >> 4;
-                const Frag<T> of = load_cols<DV>(os, 16 * wave, 32 * i, lane);
+                const Frag<T> of = load_cols<LV>(os, 16 * wave, 32 * i, lane);
                 const f32x8 w = load_steps<T>(decays.from_start + 32 * i, g) * p.scale;
                 Split<T> ow;
                 ow.set(widen(of) * w, false);
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    const Frag<T> qf = load_paired<DK>(qs, kt, 32 * i, lane);
+                    const Frag<T> qf = load_paired<LK>(qs, kt, 32 * i, lane);
 #pragma unroll
                     for (int e = 0; e < Split<T>::COUNT; ++e) grad[kt] = mma(qf, ow.part[e], grad[kt]);
                 }
@@ -461,16 +464,21 @@ __global__ __launch_bounds__(256) void heinsen_attention_decay_sum(const float *
 
 // ---- host -----------------------------------------------------------------------------------------------------
 
-template <typename T, int C, int DK, int DV> hipError_t backward_sized(const BackwardArgs &a, int64_t blocks, hipStream_t stream)
+template <typename T, int C, int DK, int DV, bool NARROW> hipError_t backward_sized(const BackwardArgs &a, int64_t blocks, hipStream_t stream)
 {
-    heinsen_attention_backward<T, C, DK, DV><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
+    heinsen_attention_backward<T, C, DK, DV, NARROW><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <typename T, int C> hipError_t backward(const BackwardArgs &a, int64_t blocks, hipStream_t stream)
 {
-    if (a.K <= 64) return a.V <= 64 ? backward_sized<T, C, 64, 64>(a, blocks, stream) : backward_sized<T, C, 64, 128>(a, blocks, stream);
-    return a.V <= 64 ? backward_sized<T, C, 128, 64>(a, blocks, stream) : backward_sized<T, C, 128, 128>(a, blocks, stream);
+    constexpr int N = 16 / (int)sizeof(T);
+    if (a.K < N || a.V < N) {
+        if (a.K > 64) return backward_sized<T, C, 128, 64, true>(a, blocks, stream);
+        return a.V <= 64 ? backward_sized<T, C, 64, 64, true>(a, blocks, stream) : backward_sized<T, C, 64, 128, true>(a, blocks, stream);
+    }
+    if (a.K <= 64) return a.V <= 64 ? backward_sized<T, C, 64, 64, false>(a, blocks, stream) : backward_sized<T, C, 64, 128, false>(a, blocks, stream);
+    return a.V <= 64 ? backward_sized<T, C, 128, 64, false>(a, blocks, stream) : backward_sized<T, C, 128, 128, false>(a, blocks, stream);
 }
 
 // Parts of the scratch, in this order.
