@@ -2,9 +2,9 @@
 // layouts in registers and LDS, and the decays within a chunk of tokens.
 //
 // A fragment holds, in each lane l = 16 g + r, the entries of row (or column) r at eight steps of the contraction: 8g..8g+7 in
-// bfloat16, 4g..4g+3 and 16+4g..16+4g+3 in float32, where they go through eight products of four steps.  An accumulator block
-// has column r and rows 4g..4g+3 in lane l.  Two neighbouring blocks of a state are such a fragment as they are, without a way
-// through LDS, if their rows stand for the right entries: paired() says which.
+// bfloat16; 4g..4g+3 and 16+4g..16+4g+3 in float32, where they go through eight products of four steps each.  An accumulator
+// block has column r and rows 4g..4g+3 in lane l, so two neighbouring blocks of a state become an operand of the next product
+// without a way through LDS (state_frag).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -43,80 +43,73 @@ __device__ static inline f32x4 mma(f32x8 a, f32x8 b, f32x4 acc)
 }
 
 template <typename T> __device__ static inline Frag<T> join(x4<T> a, x4<T> b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
-template <typename T> __device__ static inline Frag<T> to_frag(f32x4 a, f32x4 b)
+// The fragment of two accumulator blocks one above the other.
+template <typename T> __device__ static inline Frag<T> state_frag(f32x4 a, f32x4 b);
+template <> __device__ inline f32x8 state_frag<float>(f32x4 a, f32x4 b) { return join<float>(a, b); }
+template <> __device__ inline bf16x8 state_frag<__bf16>(f32x4 a, f32x4 b)
 {
-    return join<T>(__builtin_convertvector(a, x4<T>), __builtin_convertvector(b, x4<T>));
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_convertvector(a, bf16x4)), y = __builtin_bit_cast(u32x2, __builtin_convertvector(b, bf16x4));
+    u32x4 f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) { // rows 4g of a and of b in the groups of lanes g = 0..3 become rows 8g and 8g + 4
+        const auto half = __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false);
+        const auto quarter = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
+        f[i] = quarter[0];
+        f[2 + i] = quarter[1];
+    }
+    return __builtin_bit_cast(bf16x8, f);
 }
 
-// Step of the contraction that entry e of a fragment stands for, and the index that row r of block `tile` of a state has.
+// Step of the contraction that entry e of a fragment stands for.
 template <typename T> __device__ static inline int step_of(int g, int e) { return sizeof(T) == 2 ? 8 * g + e : (e >> 2) * 16 + 4 * g + (e & 3); }
-template <typename T> __device__ static inline int paired(int tile, int r)
-{
-    return sizeof(T) == 2 ? 32 * (tile >> 1) + 8 * (r >> 2) + 4 * (tile & 1) + (r & 3) : 16 * tile + r;
-}
 
-// Tiles of rows of D entries in LDS: where entry (row, col) is.
+// Tiles of rows of D entries in LDS: at(row0, r, col0, c) is the place of entry (row0 + r, col0 + c), row0 a multiple of 16 and
+// col0 of all that c may be, so that the compiler sees what of an address is constant.
 //
-// Padded: rows a few banks apart, so that sixteen lanes that read a 16-byte piece of a row each touch all banks once, and those
-// that read pieces of four rows twice at most.  Addresses are a lane's own plus a constant.
-// Swapped: no padding; the pieces of a row change places with the row's number, so that the accesses below each touch all
-// banks once.  Addresses take a few instructions: for the kernel that fills LDS.
-template <typename T_, int D_> struct Padded {
+// float32: rows four banks apart.  bfloat16: no padding; the 16-byte pieces of a row change places with the row's number, so
+// that sixteen lanes that read a piece each of sixteen rows, and half a wave that reads 32 bytes of each of the rows 0..3 and
+// 8..11 (or 4..7 and 12..15), touch all banks once.
+template <typename T_, int D_> struct Tile {
     typedef T_ T;
-    static constexpr int D = D_, PITCH = D + (sizeof(T) == 2 ? 24 : 4);
-    __device__ static int at(int row, int col) { return row * PITCH + col; }
-};
-template <typename T_, int D_> struct Swapped {
-    typedef T_ T;
-    static constexpr int D = D_, PITCH = D, N = 16 / (int)sizeof(T), PIECES = D / N;
-    static_assert(PIECES >= 8, "eight pieces to a row at least");
-    __device__ static int at(int row, int col)
+    static constexpr int D = D_, PITCH = sizeof(T) == 2 ? D : D + 4;
+    static_assert(sizeof(T) == 4 || D == 64 || D == 128, "the order of the pieces");
+    __device__ static int at(int row0, int r, int col0, int c)
     {
-        int swap;
-        if (PIECES >= 16) swap = sizeof(T) == 2 ? ((row & 3) << 2) | ((row >> 2) & 3) : row & 15;
-        else swap = sizeof(T) == 2 ? ((row & 2) << 1) | ((row >> 2) & 3) : (row >> 1) & 7;
-        return row * D + (((col / N) ^ swap) * N) + col % N;
+        if (sizeof(T) == 4) return (row0 + r) * PITCH + col0 + c;
+        const int swap = D == 128 ? ((r & 3) << 1) | (r & 8) | ((r >> 2) & 1) : (r & 2) | ((r & 8) >> 1) | ((r >> 2) & 1);
+        return row0 * D + r * D + ((((c >> 3) ^ swap) ^ (col0 >> 3)) << 3) + (c & 7);
     }
 };
 
 // Fragment of rows row0.. of a tile, contraction along the row from k0 on.
 template <typename L> __device__ static inline bf16x8 load_rows(const __bf16 *tile, int row0, int k0, int lane)
 {
-    return *reinterpret_cast<const bf16x8 *>(tile + L::at(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
+    return *reinterpret_cast<const bf16x8 *>(tile + L::at(row0, lane & 15, k0, 8 * (lane >> 4)));
 }
 template <typename L> __device__ static inline f32x8 load_rows(const float *tile, int row0, int k0, int lane)
 {
-    const int row = row0 + (lane & 15), col = k0 + 4 * (lane >> 4);
-    return join<float>(*reinterpret_cast<const f32x4 *>(tile + L::at(row, col)), *reinterpret_cast<const f32x4 *>(tile + L::at(row, col + 16)));
+    const float *const p = tile + L::at(row0, lane & 15, k0, 4 * (lane >> 4));
+    return join<float>(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 16));
 }
 
-// Fragment of columns of a tile, contraction down the rows from k0 on.
+// Fragment of columns col0.. of a tile, contraction down the rows from k0 on.
 __device__ static inline bf16x4 transposed4(const __bf16 *p)
 {
     return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                           (__attribute__((address_space(3))) i16x4 *)(const_cast<__bf16 *>(p))));
 }
-// sixteen lanes read four entries each of four rows, `apart` entries from one lane's to the next one's, and get a column each
-template <typename L> __device__ static inline bf16x8 columns(const __bf16 *tile, int col0, int apart, int k0, int lane)
+// sixteen lanes read four entries each of four rows and get a column each
+template <typename L> __device__ static inline bf16x8 load_cols(const __bf16 *tile, int col0, int k0, int lane)
 {
-    const int row = k0 + 8 * (lane >> 4) + ((lane & 15) >> 2), col = col0 + apart * (lane & 3);
-    return join<__bf16>(transposed4(tile + L::at(row, col)), transposed4(tile + L::at(row + 4, col)));
+    const int r = 8 * (lane >> 4) + ((lane & 15) >> 2), c = 4 * (lane & 3);
+    return join<__bf16>(transposed4(tile + L::at(k0, r, col0, c)), transposed4(tile + L::at(k0, r + 4, col0, c)));
 }
-template <typename L> __device__ static inline f32x8 columns(const float *tile, int col0, int, int k0, int lane)
+template <typename L> __device__ static inline f32x8 load_cols(const float *tile, int col0, int k0, int lane)
 {
     f32x8 f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = tile[L::at(k0 + step_of<float>(lane >> 4, e), col0 + (lane & 15))];
+    for (int e = 0; e < 8; ++e) f[e] = tile[L::at(k0, step_of<float>(lane >> 4, e), col0, lane & 15)];
     return f;
-}
-// columns 16 * tile.., or those that the rows of block `tile` of a state stand for
-template <typename L, typename T> __device__ static inline Frag<T> load_cols(const T *tile, int col0, int k0, int lane)
-{
-    return columns<L>(tile, col0, 4, k0, lane);
-}
-template <typename L, typename T> __device__ static inline Frag<T> load_paired(const T *tile, int block, int k0, int lane)
-{
-    return columns<L>(tile, paired<T>(block, 0), sizeof(T) == 2 ? 8 : 4, k0, lane);
 }
 
 // Eight float32 in the fragment's order of steps, from k0 on.
@@ -170,6 +163,23 @@ template <> struct Split<__bf16> {
     }
 };
 
+// Of four float32, the eight bits below those that rounding to bfloat16 keeps, and the number of such bits and the rounded
+// one.  u + 2^15 - 1 (and one more where the last bit kept is odd) carries into the upper half where the number is rounded up.
+__device__ static inline uint32_t fine_bits(f32x4 x)
+{
+    u32x4 u = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] += 0x7fffu + (u[e] >> 16 & 1u);
+    return __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0501u) | __builtin_amdgcn_perm(u[3], u[2], 0x05010c0cu);
+}
+__device__ static inline f32x4 refined(bf16x4 rounded, uint32_t fine)
+{
+    const u32x2 u = __builtin_bit_cast(u32x2, rounded);
+    const u32x4 x = {__builtin_amdgcn_perm(u[0], fine, 0x0504000cu), __builtin_amdgcn_perm(u[0], fine, 0x0706010cu),
+                     __builtin_amdgcn_perm(u[1], fine, 0x0504020cu), __builtin_amdgcn_perm(u[1], fine, 0x0706030cu)};
+    return __builtin_bit_cast(f32x4, x - 0x7f00u);
+}
+
 // x, of which the compiler does not know that it is: what is formed from it is formed here, not ahead of the loop, where the
 // addresses of all the accesses of a chunk would fill the registers.
 __device__ static inline int fresh(int x)
@@ -177,6 +187,9 @@ __device__ static inline int fresh(int x)
     asm volatile("" : "+v"(x));
     return x;
 }
+
+// x, or zero whatever x is; without a branch around what x is formed by
+__device__ static inline float kept(float x, bool keep) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & (keep ? ~0u : 0u)); }
 
 // x, the same in all lanes, in scalar registers
 __device__ static inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -223,10 +236,10 @@ template <typename L, int C, int THREADS, bool NARROW> struct TileLoad {
         step = uniform((uint32_t)stride * (uint32_t)sizeof(T));
         end = NARROW && d < N ? 0 : (uint32_t)d * (uint32_t)sizeof(T);
     }
-    // Rows past the last are zero: the hardware reads nothing past the end that it is told.
-    __device__ void load(int rows)
+    // Rows past the last are zero: the hardware reads nothing past the end that it is told.  thread: threadIdx.x.
+    __device__ void load(int rows, uint32_t thread)
     {
-        const uint32_t thread = (uint32_t)fresh((int)threadIdx.x), piece = thread % PER_ROW * 16, last = end - 16;
+        const uint32_t piece = thread % PER_ROW * 16, last = end - 16;
         const uint32_t offset = thread / PER_ROW * step + (piece < last ? piece : last);
         const __amdgpu_buffer_rsrc_t memory =
             __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(next), 0, NARROW && end == 0 ? 0 : (int)((uint32_t)(rows - 1) * step + end), 0x00020000);
@@ -254,7 +267,7 @@ template <typename L, int C, int THREADS, bool NARROW> struct TileLoad {
     __device__ bool store(T *tile, const T *base, int64_t stride, int rows, int d) const
     {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) *reinterpret_cast<u32x4 *>(tile + L::at(row(i), col())) = v[i];
+        for (int i = 0; i < COUNT; ++i) *reinterpret_cast<u32x4 *>(tile + L::at(0, row(i), 0, col())) = v[i];
         bool odd = false;
         if (NARROW && d < N && col() == 0) {
 #pragma unroll 1
@@ -262,7 +275,7 @@ template <typename L, int C, int THREADS, bool NARROW> struct TileLoad {
 #pragma unroll 1
                 for (int j = 0; j < d; ++j) {
                     const T x = base[at_row * stride + j];
-                    tile[L::at(at_row, j)] = x;
+                    tile[L::at(0, at_row, 0, j)] = x;
                     odd |= !(__builtin_fabsf((float)x) < __builtin_inff());
                 }
         }

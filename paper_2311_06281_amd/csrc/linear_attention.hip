@@ -7,7 +7,6 @@
 //     o_t = scale (e^{G_t} S^T q_t + sum_{s<=t} e^{G_t-G_s} (q_t . k_s) v_s),   S' = e^{G_C} S + sum_s e^{G_C-G_s} k_s v_s^T.
 #include "attention_tiles.hpp"
 #include "operators.hpp"
-#include <cstdlib>
 
 namespace hs {
 namespace {
@@ -18,14 +17,15 @@ struct SweepArgs {
     const void *q, *k, *v, *log_a;
     const float *s0;
     const int64_t *starts;
-    void *out;               // kOutput: out; kChunkStates: the state at each chunk's start, [B, H, chunks, DK, DV] in T
+    void *out;               // kOutput: out; kChunkStates: the state at each chunk's start, transposed, [B, H, chunks, DV, DK] in T
+    uint32_t *fine;          // kChunkStates in bfloat16: [B, H, chunks, waves, 64, DK / 16], more bits of these states
     float *sn;
     int64_t n, q_stride, k_stride, v_stride;
     int64_t segment;         // tokens of a segment, a whole number of chunks
     float *segment_state;    // [B, H, segments, K, V]: kSegment...: written; else, where there are several: the state at its start
     float *segment_decay;    // [B, H, segments]: written by kSegment...
     int H, share, K, V, segments, chunks;
-    int units, slices;       // heads and segments of all sequences; workgroups to each, DV columns of v apart
+    int units;               // heads and segments of all sequences, a workgroup to each
     float scale;
     bool per_head;
 };
@@ -39,24 +39,19 @@ template <typename F> __device__ static inline F finite(F f)
     return f;
 }
 
-// Work of a workgroup: workgroup i runs on die i % 8, and the slices of a unit, which read the same q and k, go to one die.
-__device__ static inline int unit_and_slice(int slices, int &slice)
-{
-    slice = blockIdx.x / 8 % slices;
-    return blockIdx.x / (8 * slices) * 8 + blockIdx.x % 8;
-}
-
-// A workgroup takes one segment of one head's tokens and goes through its chunks, DV columns of the state in registers, sixteen
-// to a wave.  kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
+// A workgroup takes one segment of one head's tokens and goes through its chunks, the state in registers, sixteen columns to a
+// wave.  The heads' first segments come first, then their second ones and so on, so that ragged sequences leave no die idle.
+// kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
 // (k, v) and gives the segment's own part of the gradient of the state it starts from.
-template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW>
-__global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p)
+template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW, bool ROOMY>
+__global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep(SweepArgs p)
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
     constexpr bool BACK = SWEEP == kSegmentGradient;
-    typedef Padded<T, DK> LK;
-    typedef Padded<T, DV> LV;
-    typedef Padded<T, C> LC;
+    constexpr bool FEW = sizeof(T) == 2 && DK == 128 && !ROOMY && (SWEEP == kOutput || DV == 64); // registers to keep addresses in
+    typedef Tile<T, DK> LK;
+    typedef Tile<T, DV> LV;
+    typedef Tile<T, C> LC;
     __shared__ __align__(16) T ks[C * LK::PITCH];
     __shared__ __align__(16) T vs[C * LV::PITCH];
     __shared__ __align__(16) T qs[SWEEP == kOutput ? C * LK::PITCH : 16];
@@ -65,33 +60,30 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
     __shared__ int not_finite[2]; // of even and odd chunks
 
     const int lane0 = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), r = lane0 & 15, g = lane0 >> 4;
-    int slice;
-    const int unit = unit_and_slice(p.slices, slice);
-    if (unit >= p.units) return;
-    const int seg = unit % p.segments, bh = unit / p.segments, h = bh % p.H, b = bh / p.H;
+    const int heads = gridDim.x / p.segments, seg = blockIdx.x / heads, bh = blockIdx.x % heads, h = bh % p.H, b = bh / p.H;
     int64_t first;
     const int64_t len = uniform_sequence(p.starts, p.n, b, first);
     const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
     if (begin >= len && (seg > 0 || SWEEP != kOutput)) return;
 
-    const int v0 = slice * DV, V = p.V - v0 < DV ? p.V - v0 : DV; // of this workgroup's columns
+    const int V = p.V;
     const T *const k = static_cast<const T *>(p.k) + first * p.k_stride + (int64_t)(h / p.share) * p.K;
     const T *const q = static_cast<const T *>(p.q) + first * p.q_stride + (int64_t)(h / p.share) * p.K;
-    const T *const v = static_cast<const T *>(p.v) + first * p.v_stride + (int64_t)h * p.V + v0;
+    const T *const v = static_cast<const T *>(p.v) + first * p.v_stride + (int64_t)h * p.V;
     const T *const log_a = static_cast<const T *>(p.log_a);
     const int col = 16 * wave + r; // of v, of this lane's entries of the state
 
     f32x4 state[KT];
     const bool segment_start = (SWEEP == kOutput || SWEEP == kChunkStates) && p.segments > 1 && begin < len;
-    const float *const from = segment_start ? p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0
-                              : (SWEEP == kOutput || SWEEP == kChunkStates) && p.s0 ? p.s0 + (int64_t)bh * p.K * p.V + v0 : nullptr;
+    const float *const from = segment_start ? p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V
+                              : (SWEEP == kOutput || SWEEP == kChunkStates) && p.s0 ? p.s0 + (int64_t)bh * p.K * p.V : nullptr;
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
         state[i] = f32x4{0, 0, 0, 0};
         if (from)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int row = paired<T>(i, 4 * g + e);
+                const int row = 16 * i + 4 * g + e;
                 const float x = from[(uint32_t)((row < p.K ? row : 0) * p.V + (col < V ? col : 0))];
                 state[i][e] = row < p.K && col < V ? x : 0.0f;
             }
@@ -108,12 +100,13 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
     if (SWEEP == kOutput) next_q.start(q + chunk_start(0) * p.q_stride, p.q_stride, p.K);
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_k.load(rows);
+        const uint32_t thread = (uint32_t)(64 * wave + fresh(lane0));
+        next_k.load(rows, thread);
         next_k.move(BACK ? -C : C);
-        next_v.load(rows);
+        next_v.load(rows, thread);
         next_v.move(BACK ? -C : C);
         if (SWEEP == kOutput) {
-            next_q.load(rows);
+            next_q.load(rows, thread);
             next_q.move(C);
         }
         if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + fresh(lane0 < rows ? lane0 : 0)) * p.H + h];
@@ -143,11 +136,12 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
         if (threadIdx.x == 0) not_finite[(chunk + 1) & 1] = 0;
         if (chunk + 1 < chunks) request(chunk_start(chunk + 1));
 
+        f32x4 o[SWEEP == kOutput ? TT : 1]; // of the outputs; rows: columns of v, columns: tokens
         if (SWEEP == kOutput) {
             // the weights of the chunk's tokens for one another, scale e^{G_t-G_s} q_t . k_s, in tiles of 16 x 16: this wave's
             // are those of tokens t in one row of tiles
             const int tt = wave % TT;
-            const int lane = lane0;
+            const int lane = FEW ? fresh(lane0) : lane0, r = lane & 15, g = lane >> 4;
             Frag<T> qf[DK / 32];
 #pragma unroll
             for (int i = 0; i < DK / 32; ++i) qf[i] = load_rows<LK>(qs, 16 * tt, 32 * i, lane);
@@ -162,25 +156,44 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float w = __builtin_amdgcn_exp2f((whole_t - whole[e]) + (part_t - part[e])) * p.scale;
-                        acc[e] = 16 * st + 4 * g + e <= 16 * tt + r ? acc[e] * w : 0.0f;
+                        acc[e] = kept(acc[e] * w, 16 * st + 4 * g + e <= 16 * tt + r);
                     }
                 }
-                *reinterpret_cast<x4<T> *>(ps + LC::at(16 * tt + r, 16 * st + 4 * g)) = __builtin_convertvector(acc, x4<T>);
+                *reinterpret_cast<x4<T> *>(ps + LC::at(16 * tt, r, 16 * st, 4 * g)) = __builtin_convertvector(acc, x4<T>);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            // what the tokens get from the state, which needs no other wave's weights
+#pragma unroll
+            for (int t = 0; t < TT; ++t) o[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < DK / 32; ++i) {
+                const Frag<T> sf = state_frag<T>(state[2 * i], state[2 * i + 1]);
+#pragma unroll
+                for (int t = 0; t < TT; ++t) o[t] = mma(sf, load_rows<LK>(qs, 16 * t, 32 * i, lane), o[t]);
+                __builtin_amdgcn_sched_barrier(0); // loads of what follows would only take registers here
+            }
+#pragma unroll
+            for (int t = 0; t < TT; ++t) o[t] *= decays.from_start[16 * t + r] * p.scale;
             __syncthreads();
         }
         if (SWEEP == kChunkStates) {
-            T *const to = static_cast<T *>(p.out) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV * p.slices) + v0 * DK;
-            const uint32_t at = (uint32_t)fresh(col * DK + paired<T>(0, 4 * g));
+            T *const to = static_cast<T *>(p.out) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV);
+            const uint32_t at = (uint32_t)fresh(col * DK + 4 * g);
 #pragma unroll
             for (int i = 0; i < KT; ++i)
-                *reinterpret_cast<x4<T> *>(to + at + paired<T>(i, 0)) = __builtin_convertvector(state[i], x4<T>);
+                *reinterpret_cast<x4<T> *>(to + at + 16 * i) = __builtin_convertvector(state[i], x4<T>);
+            if (sizeof(T) == 2) {
+                uint32_t *const fine = p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4) + (uint32_t)fresh((64 * wave + lane0) * KT);
+#pragma unroll
+                for (int i = 0; i < KT; i += 4)
+                    *reinterpret_cast<u32x4 *>(fine + i) = u32x4{fine_bits(state[i]), fine_bits(state[i + 1]), fine_bits(state[i + 2]), fine_bits(state[i + 3])};
+            }
         }
 
         __builtin_amdgcn_sched_barrier(0);
         Frag<T> vf[C / 32];
         {
-            const int lane = lane0;
+            const int lane = FEW ? fresh(lane0) : lane0;
 #pragma unroll
             for (int i = 0; i < C / 32; ++i) vf[i] = load_cols<LV>(vs, 16 * wave, 32 * i, lane);
         }
@@ -189,34 +202,28 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
             if (odd_values)
 #pragma unroll
                 for (int i = 0; i < C / 32; ++i) vf[i] = finite(vf[i]);
-            const int lane = lane0;
-            T *const out_base = static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V + v0;
-            const uint32_t out_step = (uint32_t)(p.H * p.V) * (uint32_t)sizeof(T), out_offset = r * out_step + (16 * wave + 4 * g) * (uint32_t)sizeof(T);
+            const int lane = FEW ? fresh(lane0) : lane0;
+            T *const out_base = static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V;
+            const uint32_t out_step = (uint32_t)(p.H * p.V) * (uint32_t)sizeof(T), out_offset = (uint32_t)fresh(r) * out_step + (16 * wave + 4 * (uint32_t)fresh(g)) * (uint32_t)sizeof(T);
             const __amdgpu_buffer_rsrc_t out =
                 __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(uniform((uint64_t)reinterpret_cast<uintptr_t>(out_base))), 0,
                                                   (int)((uint32_t)(rows - 1) * out_step + DV * (uint32_t)sizeof(T)), 0x00020000);
-            Frag<T> sf[DK / 32];
 #pragma unroll
-            for (int i = 0; i < DK / 32; ++i) sf[i] = to_frag<T>(state[2 * i], state[2 * i + 1]);
+            for (int i = 0; i < C / 32; ++i)
+#pragma unroll
+                for (int t = 2 * i; t < TT; ++t) o[t] = mma(vf[i], load_rows<LC>(ps, 16 * t, 32 * i, lane), o[t]);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
-                f32x4 o = {0, 0, 0, 0}; // rows: columns of v, columns: tokens
-#pragma unroll
-                for (int i = 0; i < DK / 32; ++i) o = mma(sf[i], load_rows<LK>(qs, 16 * t, 32 * i, lane), o);
-                o *= decays.from_start[16 * t + r] * p.scale;
-#pragma unroll
-                for (int i = 0; i <= t / 2; ++i) o = mma(vf[i], load_rows<LC>(ps, 16 * t, 32 * i, lane), o);
-                if (V == DV) { // tokens past the last are not written: the hardware writes nothing past the end that it is told
-                    buffer_store(__builtin_convertvector(o, x4<T>), out, out_offset, out_step * (16 * t));
-                } else if (16 * t + r < rows) {
-                    store4(out_base, (uint32_t)(16 * t + fresh(r)) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, V, o);
-                }
-                __builtin_amdgcn_sched_barrier(0); // loads of what follows would only take registers here
+                if (V == DV) // tokens past the last are not written: the hardware writes nothing past the end that it is told
+                    buffer_store(__builtin_convertvector(o[t], x4<T>), out, out_offset, out_step * (16 * t));
+                else if (16 * t + r < rows)
+                    store4(out_base, (uint32_t)(16 * t + fresh(r)) * (uint32_t)(p.H * p.V), 16 * wave + 4 * g, V, o[t]);
             }
+            __builtin_amdgcn_sched_barrier(0);
             if (odd_values) {
                 // an infinite or NaN v_s has no part in the tokens before it, where its zero weight would make it NaN: such
                 // values were left out above and are added to the tokens that see them
-                T *const out = static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V + v0;
+                T *const out = static_cast<T *>(p.out) + ((first + t0) * p.H + h) * p.V;
 #pragma unroll 1
                 for (int t = fresh(r); t < rows; t += 16)
 #pragma unroll 1
@@ -224,8 +231,8 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
                         float more = 0.0f;
 #pragma unroll 1
                         for (int s = 0; s <= t; ++s) {
-                            const float x = to_float(vs[LV::at(s, c)]);
-                            if (!(__builtin_fabsf(x) < __builtin_inff())) more += to_float(ps[LC::at(t, s)]) * x;
+                            const float x = to_float(vs[LV::at(0, s, 0, c)]);
+                            if (!(__builtin_fabsf(x) < __builtin_inff())) more += to_float(ps[LC::at(0, t, 0, s)]) * x;
                         }
                         T *const to = out + (uint32_t)t * (uint32_t)(p.H * p.V) + c;
                         if (more != 0.0f) *to = (T)(to_float(*to) + more);
@@ -239,7 +246,7 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
         const float decay = decays.total;
 #pragma unroll
         for (int i = 0; i < KT; ++i) state[i] *= decay;
-        const int lane = lane0;
+        const int lane = FEW ? fresh(lane0) : lane0;
 #pragma unroll
         for (int i = 0; i < C / 32; ++i) {
             f32x8 w = load_steps<T>((BACK ? decays.from_start : decays.to_end) + 32 * i, lane >> 4);
@@ -247,11 +254,16 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
             // v scaled by its decay enters unrounded
             Split<T> vw;
             vw.set(widen(vf[i]) * w, odd_values);
+            constexpr int SIDE = 2; // sums side by side
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const Frag<T> kf = load_paired<LK>(ks, kt, 32 * i, lane);
+            for (int kt = 0; kt < KT; kt += SIDE) {
+                Frag<T> kf[SIDE];
 #pragma unroll
-                for (int e = 0; e < Split<T>::COUNT; ++e) state[kt] = mma(kf, vw.part[e], state[kt]);
+                for (int j = 0; j < SIDE; ++j) kf[j] = load_cols<LK>(ks, 16 * (kt + j), 32 * i, lane);
+#pragma unroll
+                for (int e = 0; e < Split<T>::COUNT; ++e)
+#pragma unroll
+                    for (int j = 0; j < SIDE; ++j) state[kt + j] = mma(kf[j], vw.part[e], state[kt + j]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -262,7 +274,7 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
             for (int i = 0; i < KT; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (paired<T>(i, 4 * g + e) >= p.K) state[i][e] = 0.0f;
+                    if (16 * i + 4 * g + e >= p.K) state[i][e] = 0.0f;
         }
         __syncthreads();
     }
@@ -270,17 +282,17 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_sweep(SweepArgs p
     const int row0 = fresh(4 * g), col0 = fresh(col);
     float *to = nullptr;
     if (SWEEP == kSegmentState || SWEEP == kSegmentGradient) {
-        to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V + v0;
-        if (threadIdx.x == 0 && slice == 0) p.segment_decay[(int64_t)bh * p.segments + seg] = __builtin_amdgcn_exp2f((float)total);
+        to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V;
+        if (threadIdx.x == 0) p.segment_decay[(int64_t)bh * p.segments + seg] = __builtin_amdgcn_exp2f((float)total);
     } else if (SWEEP == kOutput && p.sn && end == len) {
-        to = p.sn + (int64_t)bh * p.K * p.V + v0;
+        to = p.sn + (int64_t)bh * p.K * p.V;
     }
     if (to)
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int row = paired<T>(i, row0 + e);
+                const int row = 16 * i + row0 + e;
                 if (row < p.K && col0 < V) to[(uint32_t)(row * p.V + col0)] = state[i][e];
             }
 }
@@ -402,11 +414,9 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 
 template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 : 32; }
 
-template <typename T, int SWEEP, int DK, int DV, bool NARROW> hipError_t sweep_sized(SweepArgs &a, hipStream_t stream)
+template <typename T, int SWEEP, int DK, int DV, bool NARROW, bool ROOMY = false> hipError_t sweep_sized(SweepArgs &a, hipStream_t stream)
 {
-    a.slices = (a.V + DV - 1) / DV;
-    const int64_t blocks = ((int64_t)a.units + 7) / 8 * 8 * a.slices;
-    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP, NARROW><<<dim3((unsigned)blocks), 4 * DV, 0, stream>>>(a);
+    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP, NARROW, ROOMY><<<dim3((unsigned)a.units), 4 * DV, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -418,7 +428,10 @@ template <typename T, int SWEEP> hipError_t sweep(SweepArgs &a, hipStream_t stre
         return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, true>(a, stream) : sweep_sized<T, SWEEP, 64, 128, true>(a, stream);
     }
     if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, false>(a, stream) : sweep_sized<T, SWEEP, 64, 128, false>(a, stream);
-    return a.V <= 64 ? sweep_sized<T, SWEEP, 128, 64, false>(a, stream) : sweep_sized<T, SWEEP, 128, 128, false>(a, stream);
+    if (a.V <= 64) return sweep_sized<T, SWEEP, 128, 64, false>(a, stream);
+    // where there is one workgroup to a compute unit only, its waves can have all registers
+    if (SWEEP == kOutput && a.units < 2 * compute_units()) return sweep_sized<T, SWEEP, 128, 128, false, SWEEP == kOutput>(a, stream);
+    return sweep_sized<T, SWEEP, 128, 128, false>(a, stream);
 }
 
 SweepArgs sweep_args(const AttentionCall &c, const Segments &s)
@@ -460,12 +473,18 @@ template <typename T> hipError_t step(const AttentionCall &c)
 
 } // namespace
 
-Segments attention_segments(const AttentionCall &c)
+// A head's segments go side by side, at the cost of reading k and v twice and of a state for each segment to be joined.
+// Microseconds of all kernels of a call, by segments of a head; bfloat16, K = V = 128 where nothing else is said:
+//     256 heads, 16384 tokens                     1: 1412   2: 1929
+//     128 heads, ragged lengths up to 4096        2: 236    4: 206    6: 175    8: 203
+//     4 heads of K = V = 48, float32, 131072      64: 338   128: 259  192: 245  256: 237
+//     64 heads, 4096, backward                    4: 459    8: 477
+//     60 heads of K = 55, V = 77, ragged up to 3001, backward    5: 187   6: 164
+// Of the backward pass two workgroups fit a compute unit at K, V <= 64 only.
+Segments attention_segments(const AttentionCall &c, bool back)
 {
-    // two workgroups to a compute unit at least, while a segment stays long against the states it adds
-    static const int per_unit = getenv("HS_PU") ? atoi(getenv("HS_PU")) : 2;
-    const int64_t heads = (int64_t)c.B * c.H, want = per_unit * compute_units();
-    int64_t count = heads >= want ? 1 : (want + heads - 1) / heads;
+    const int64_t heads = (int64_t)c.B * c.H, per_unit = !back ? 3 : c.starts || (c.K <= 64 && c.V <= 64) ? 2 : 1, want = per_unit * compute_units();
+    int64_t count = heads >= compute_units() ? 1 : (want + heads - 1) / heads;
     const int64_t most = (c.n + 511) / 512;
     if (count > most) count = most;
     Segments s;
@@ -499,22 +518,22 @@ hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, b
     return chain(back, a.segment_state, a.segment_decay, back ? c.grad_sn : c.s0, c, s);
 }
 
-hipError_t attention_chunk_states(const AttentionCall &c, const Segments &s, float *segment_state, void *states, int chunks)
+hipError_t attention_chunk_states(const AttentionCall &c, const Segments &s, float *segment_state, void *states, uint32_t *fine, int chunks)
 {
     SweepArgs a = sweep_args(c, s);
     a.segment_state = segment_state;
-    a.out = states, a.chunks = chunks;
+    a.out = states, a.fine = fine, a.chunks = chunks;
     return c.bf16 ? sweep<__bf16, kChunkStates>(a, c.stream) : sweep<float, kChunkStates>(a, c.stream);
 }
 
 int attention_chunk_tokens(bool bf16) { return bf16 ? chunk_tokens<__bf16>() : chunk_tokens<float>(); }
 
-size_t attention_scratch(const AttentionCall &c) { return c.n <= kFewTokens ? 0 : segment_scratch(c, attention_segments(c)); }
+size_t attention_scratch(const AttentionCall &c) { return c.n <= kFewTokens ? 0 : segment_scratch(c, attention_segments(c, false)); }
 
 hipError_t attention_launch(const AttentionCall &c, void *scratch)
 {
     if (c.n <= kFewTokens) return c.bf16 ? step<__bf16>(c) : step<float>(c);
-    const Segments s = attention_segments(c);
+    const Segments s = attention_segments(c, false);
     if (s.count > 1) {
         const hipError_t e = attention_segment_states(c, s, false, scratch);
         if (e != hipSuccess) return e;

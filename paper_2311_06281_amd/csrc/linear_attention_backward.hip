@@ -23,6 +23,7 @@ struct BackwardArgs {
     const float *grad_sn;
     const int64_t *starts;
     const void *states;           // [B, H, chunks, DV, DK] in T: the state at each chunk's start, transposed
+    const uint32_t *fine;         // bfloat16: [B, H, chunks, waves, 64, DK / 16] more bits of these states, in the order of a wave's registers
     const float *segment_grad;    // [B, H, segments, K, V]: where there are several, the gradient of the state at each one's end
     void *grad_q, *grad_k;        // T, or float for each head of v where heads share q and k
     void *grad_v, *grad_log_a;    // grad_log_a: T, or float [tokens, H] with per_head, or null
@@ -40,22 +41,22 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
     constexpr bool STAGED = sizeof(T) == 2;        // the chunk's first state goes through LDS; in float32 there is no room
-    typedef Swapped<T, DK> LK;
-    typedef Swapped<T, DV> LV;
-    typedef Swapped<T, C> LC;
-    __shared__ __align__(16) T qs[C * DK];
-    __shared__ __align__(16) T ks[C * DK];
-    __shared__ __align__(16) T vs[C * DV];
-    __shared__ __align__(16) T os[C * DV];  // grad_out
-    __shared__ __align__(16) T rs[DV * DK]; // R transposed
-    __shared__ __align__(16) T ss[STAGED ? DV * DK : 16]; // S transposed
-    __shared__ __align__(16) T ps[C * C];   // P transposed: [s][t]
-    __shared__ __align__(16) T ds[C * C];   // D transposed
+    typedef Tile<T, DK> LK;
+    typedef Tile<T, DV> LV;
+    typedef Tile<T, C> LC;
+    __shared__ __align__(16) T qs[C * LK::PITCH];
+    __shared__ __align__(16) T ks[C * LK::PITCH];
+    __shared__ __align__(16) T vs[C * LV::PITCH];
+    __shared__ __align__(16) T os[C * LV::PITCH];  // grad_out
+    __shared__ __align__(16) T rs[DV * LK::PITCH]; // R transposed
+    __shared__ __align__(16) T ss[STAGED ? DV * LK::PITCH : 16]; // S transposed
+    __shared__ __align__(16) T ps[C * LC::PITCH];   // P transposed: [s][t]
+    __shared__ __align__(16) T ds[C * LC::PITCH];   // D transposed
     __shared__ Decays<C> decays;
     __shared__ float xs[KT][C], ys[KT][C], pair_rows[TT][C], pair_cols[TT][C], spans[WAVES];
 
     const int lane0 = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), r = lane0 & 15, g = lane0 >> 4;
-    const int seg = blockIdx.x % p.segments, bh = blockIdx.x / p.segments, h = bh % p.H, b = bh / p.H;
+    const int heads = gridDim.x / p.segments, seg = blockIdx.x / heads, bh = blockIdx.x % heads, h = bh % p.H, b = bh / p.H;
     int64_t first;
     const int64_t len = uniform_sequence(p.starts, p.n, b, first);
     const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
@@ -76,7 +77,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int row = paired<T>(i, 4 * g + e);
+            const int row = 16 * i + 4 * g + e;
             grad[i][e] = 0.0f;
             if (from) {
                 const float x = from[(uint32_t)((row < p.K ? row : 0) * p.V + (col < p.V ? col : 0))];
@@ -98,16 +99,17 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     if (STAGED) next_s.start(state_of(last), DK, DK);
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
-        next_q.load(rows);
+        const uint32_t thread = (uint32_t)(64 * wave + fresh(lane0));
+        next_q.load(rows, thread);
         next_q.move(-C);
-        next_k.load(rows);
+        next_k.load(rows, thread);
         next_k.move(-C);
-        next_v.load(rows);
+        next_v.load(rows, thread);
         next_v.move(-C);
-        next_o.load(rows);
+        next_o.load(rows, thread);
         next_o.move(-C);
         if (STAGED) {
-            next_s.load(DV);
+            next_s.load(DV, thread);
             next_s.move(-DV);
         }
         if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + fresh(lane0 < rows ? lane0 : 0)) * p.H + h];
@@ -129,10 +131,15 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         if (wave == 0) write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
 #pragma unroll
         for (int i = 0; i < KT; ++i)
-            *reinterpret_cast<x4<T> *>(rs + LK::at(col, paired<T>(i, 4 * g))) = __builtin_convertvector(grad[i], x4<T>);
+            *reinterpret_cast<x4<T> *>(rs + LK::at(16 * wave, r, 16 * i, 4 * g)) = __builtin_convertvector(grad[i], x4<T>);
         __syncthreads();
-        if (chunk > 0) request(t0 - C);
         const T *const state = state_of(t0);
+        u32x4 fine[STAGED ? KT / 4 : 1];
+        if (STAGED)
+#pragma unroll
+            for (int i = 0; i < KT / 4; ++i)
+                fine[i] = *reinterpret_cast<const u32x4 *>(p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4) + (uint32_t)fresh((64 * wave + lane0) * KT) + 4 * i);
+        if (chunk > 0) request(t0 - C);
 
         // P, D and the pairs' sums, in tiles of 16 x 16 on and below the diagonal, and zeros beside it where a product
         // takes two tiles at a time
@@ -154,11 +161,11 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 for (int e = 0; e < 4; ++e) {
                     const int t = 16 * tt + 4 * g + e;
                     const float w = __builtin_amdgcn_exp2f((decays.whole[t] - whole_s) + (decays.part[t] - part_s)) * p.scale;
-                    const float pair = s < t ? pt[e] * w * dt[e] : 0.0f;
+                    const float pair = kept(pt[e] * w * dt[e], s < t);
                     below += pair;
                     across[e] = pair;
-                    pt[e] = s <= t ? pt[e] * w : 0.0f;
-                    dt[e] = s <= t ? dt[e] * w : 0.0f;
+                    pt[e] = kept(pt[e] * w, s <= t);
+                    dt[e] = kept(dt[e] * w, s <= t);
                 }
                 below += __shfl_xor(below, 16);
                 below += __shfl_xor(below, 32);
@@ -169,8 +176,8 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                     for (int e = 0; e < 4; ++e) across[e] += __shfl_xor(across[e], by);
                 if (r == 0) *reinterpret_cast<f32x4 *>(&pair_rows[st][16 * tt + 4 * g]) = across;
             }
-            *reinterpret_cast<x4<T> *>(ps + LC::at(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(pt, x4<T>);
-            *reinterpret_cast<x4<T> *>(ds + LC::at(16 * st + r, 16 * tt + 4 * g)) = __builtin_convertvector(dt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ps + LC::at(16 * st, r, 16 * tt, 4 * g)) = __builtin_convertvector(pt, x4<T>);
+            *reinterpret_cast<x4<T> *>(ds + LC::at(16 * st, r, 16 * tt, 4 * g)) = __builtin_convertvector(dt, x4<T>);
         }
         __syncthreads();
 
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
             const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
             Frag<T> rf[DK / 32];
 #pragma unroll
-            for (int i = 0; i < DK / 32; ++i) rf[i] = to_frag<T>(grad[2 * i], grad[2 * i + 1]);
+            for (int i = 0; i < DK / 32; ++i) rf[i] = state_frag<T>(grad[2 * i], grad[2 * i + 1]);
 #pragma unroll
             for (int st = 0; st < TT; ++st) {
                 f32x4 acc = {0, 0, 0, 0};
@@ -215,7 +222,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
                 for (int i = 0; i < DV / 32; ++i) acc = mma(sf[i], load_rows<LV>(os, 16 * t, 32 * i, lane), acc);
                 acc *= decays.from_start[token] * p.scale;
-                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + LK::at(token, 16 * kt + 4 * g));
+                x4<T> own = *reinterpret_cast<const x4<T> *>(qs + LK::at(16 * t, r, 16 * kt, 4 * g));
                 float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
@@ -237,7 +244,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
                 for (int i = 0; i < DV / 32; ++i) acc = mma(rf[i], load_rows<LV>(vs, 16 * t, 32 * i, lane), acc);
                 acc *= decays.to_end[token];
-                own = *reinterpret_cast<const x4<T> *>(ks + LK::at(token, 16 * kt + 4 * g));
+                own = *reinterpret_cast<const x4<T> *>(ks + LK::at(16 * t, r, 16 * kt, 4 * g));
                 sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += acc[e] * to_float(own[e]);
@@ -254,16 +261,17 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 __builtin_amdgcn_sched_barrier(0); // loads of the next tokens would only take registers here
             }
         }
-        // <R, S>, and R at the chunk's start
+        // <R, S>, in which nearly all of a long memory's decay gradient is, and R at the chunk's start
         {
             const float decay = decays.total;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < KT; ++i) {
-                const x4<T> s = STAGED ? *reinterpret_cast<const x4<T> *>(ss + LK::at(col, paired<T>(i, 4 * g)))
-                                       : *reinterpret_cast<const x4<T> *>(state + col * DK + paired<T>(i, 4 * g));
+                f32x4 s;
+                if (STAGED) s = refined(*reinterpret_cast<const bf16x4 *>(ss + LK::at(16 * wave, r, 16 * i, 4 * g)), fine[i / 4][i % 4]);
+                else s = *reinterpret_cast<const f32x4 *>(state + col * DK + 16 * i + 4 * g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += grad[i][e] * to_float(s[e]);
+                for (int e = 0; e < 4; ++e) sum += grad[i][e] * s[e];
                 grad[i] *= decay;
             }
 #pragma unroll
@@ -276,11 +284,16 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
                 const f32x8 w = load_steps<T>(decays.from_start + 32 * i, g) * p.scale;
                 Split<T> ow;
                 ow.set(widen(of) * w, false);
+                constexpr int SIDE = 4; // sums side by side
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const Frag<T> qf = load_paired<LK>(qs, kt, 32 * i, lane);
+                for (int kt = 0; kt < KT; kt += SIDE) {
+                    Frag<T> qf[SIDE];
 #pragma unroll
-                    for (int e = 0; e < Split<T>::COUNT; ++e) grad[kt] = mma(qf, ow.part[e], grad[kt]);
+                    for (int j = 0; j < SIDE; ++j) qf[j] = load_cols<LK>(qs, 16 * (kt + j), 32 * i, lane);
+#pragma unroll
+                    for (int e = 0; e < Split<T>::COUNT; ++e)
+#pragma unroll
+                        for (int j = 0; j < SIDE; ++j) grad[kt + j] = mma(qf[j], ow.part[e], grad[kt + j]);
                 }
             }
         }
@@ -317,7 +330,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         for (int i = 0; i < KT; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int row = paired<T>(i, 4 * g + e);
+                const int row = 16 * i + 4 * g + e;
                 if (row < p.K && col < p.V) to[(uint32_t)(row * p.V + col)] = grad[i][e];
             }
     }
@@ -485,22 +498,23 @@ template <typename T, int C> hipError_t backward(const BackwardArgs &a, int64_t 
 struct Parts {
     Segments segments;
     int chunks; // of the longest sequence
-    size_t states, gradients, chunk_states, shared, decays, all;
+    size_t states, gradients, chunk_states, fine, shared, decays, all;
 };
 
 Parts parts(const AttentionCall &c)
 {
     Parts s = {};
     const bool few = c.n <= kFewTokens;
-    s.segments = few ? Segments{c.n, 1} : attention_segments(c);
+    s.segments = few ? Segments{c.n, 1} : attention_segments(c, true);
     const size_t size = c.bf16 ? 2 : 4, heads = (size_t)c.B * c.H, tokens = (size_t)c.B * c.n;
     const int C = attention_chunk_tokens(c.bf16);
     s.chunks = (int)((c.n + C - 1) / C);
     s.states = s.gradients = segment_scratch(c, s.segments);
     s.chunk_states = few ? 0 : align_up(heads * s.chunks * (c.K <= 64 ? 64 : 128) * (c.V <= 64 ? 64 : 128) * size, 256);
+    s.fine = c.bf16 ? s.chunk_states / 2 : 0;
     s.shared = c.share > 1 ? align_up(tokens * c.H * c.K * sizeof(float), 256) : 0;
     s.decays = c.per_head && c.grad_log_a ? align_up(tokens * c.H * sizeof(float), 256) : 0;
-    s.all = s.states + s.gradients + s.chunk_states + 2 * s.shared + s.decays;
+    s.all = s.states + s.gradients + s.chunk_states + s.fine + 2 * s.shared + s.decays;
     return s;
 }
 
@@ -530,7 +544,8 @@ hipError_t attention_backward_launch(const AttentionCall &c, void *scratch)
     float *const segment_state = reinterpret_cast<float *>(at);
     float *const segment_grad = reinterpret_cast<float *>(at += s.states);
     void *const states = at += s.gradients;
-    float *const shared_q = reinterpret_cast<float *>(at += s.chunk_states);
+    uint32_t *const fine = reinterpret_cast<uint32_t *>(at += s.chunk_states);
+    float *const shared_q = reinterpret_cast<float *>(at += s.fine);
     float *const shared_k = reinterpret_cast<float *>(at += s.shared);
     float *const decays = reinterpret_cast<float *>(at += s.shared);
 
@@ -540,12 +555,12 @@ hipError_t attention_backward_launch(const AttentionCall &c, void *scratch)
         e = attention_segment_states(c, s.segments, false, segment_state);
         if (e == hipSuccess) e = attention_segment_states(c, s.segments, true, segment_grad);
     }
-    if (e == hipSuccess && !few) e = attention_chunk_states(c, s.segments, segment_state, states, s.chunks);
+    if (e == hipSuccess && !few) e = attention_chunk_states(c, s.segments, segment_state, states, fine, s.chunks);
     if (e != hipSuccess) return e;
 
     BackwardArgs a = {};
     a.q = c.q, a.k = c.k, a.v = c.v, a.log_a = c.log_a, a.grad_out = c.grad_out, a.grad_sn = c.grad_sn, a.starts = c.starts;
-    a.states = states, a.segment_grad = segment_grad;
+    a.states = states, a.fine = fine, a.segment_grad = segment_grad;
     a.grad_q = c.share > 1 ? shared_q : c.grad_q, a.grad_k = c.share > 1 ? shared_k : c.grad_k, a.grad_v = c.grad_v;
     a.grad_log_a = c.per_head && c.grad_log_a ? decays : c.grad_log_a;
     a.grad_s0 = c.grad_s0;
