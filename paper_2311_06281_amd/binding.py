@@ -45,7 +45,7 @@ EXPORTS = ("heinsen_scan", "heinsen_scan_static", "heinsen_status_string", "hein
            "heinsen_linear_attention_backward", "heinsen_block_norm", "heinsen_block_norm_backward")
 
 _lib = None
-_call = None  # the scan entry points without ctypes (csrc/call.c), once the library is loaded
+_call = None  # the scan's and the operators' entry points without ctypes (csrc/call.c), once the library is loaded
 _loading = threading.Lock()
 
 
@@ -112,7 +112,10 @@ def _open():
     lib.heinsen_block_norm.restype = ci
     lib.heinsen_block_norm_backward.argtypes = [vp] * 14 + [i64] * 4 + [f32, u32, vp]
     lib.heinsen_block_norm_backward.restype = ci
-    call.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.heinsen_scan, lib.heinsen_scan_static)))
+    at = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+    call.bind(at(lib.heinsen_scan), at(lib.heinsen_scan_static))
+    call.bind_operators(at(lib.heinsen_linear_attention), at(lib.heinsen_linear_attention_backward), at(lib.heinsen_block_norm),
+                        at(lib.heinsen_block_norm_backward))
     return lib, call
 
 
@@ -120,14 +123,15 @@ class _Converted:
     """In the call module's place where it has not been built, or for another Python."""
 
     @staticmethod
-    def bind(scan, scan_static):
+    def bind(*addresses):
         pass
 
     @staticmethod
     def scan(*args):
         return NotImplemented
 
-    scan_static = scan
+    scan_static = linear_attention = linear_attention_backward = block_norm = block_norm_backward = scan
+    bind_operators = bind
 
 
 def _native():
@@ -278,11 +282,15 @@ def heinsen_sequential(a, b, x0, out, n: int, stream=None) -> None:
 
 
 def _raise_for(st: int) -> None:
-    if st != HEINSEN_OK:
-        msg = heinsen_status_string(st)
-        if st in (HEINSEN_ERR_HIP, HEINSEN_ERR_ALLOC):
-            msg += f", hipError_t {heinsen_last_hip_error()}"
-        raise HeinsenError(st, msg)
+    msg = heinsen_status_string(st)
+    if st in (HEINSEN_ERR_HIP, HEINSEN_ERR_ALLOC):
+        msg += f", hipError_t {heinsen_last_hip_error()}"
+    raise HeinsenError(st, msg)
+
+
+def _convert_operator(fn, pointers, numbers, real, flags, stream) -> int:
+    """Calls an operator's entry point with arguments of any kind.  Tensors, plain numbers and a torch stream do not come here."""
+    return int(fn(*map(_addr, pointers), *map(int, numbers), float(real), int(flags), _stream_handle(stream)))
 
 
 def heinsen_linear_attention(q, k, v, log_a, s0, out, sn, B: int, n: int, H: int, K: int, V: int, scale: float, flags: int, stream=None, *,
@@ -291,35 +299,54 @@ def heinsen_linear_attention(q, k, v, log_a, s0, out, sn, B: int, n: int, H: int
     include/heinsen.h.  Asynchronous on `stream`.
 
     Hk: heads of q and k (default: H).  starts: device int64 [B + 1], where sequences of different lengths start."""
-    _raise_for(load().heinsen_linear_attention(
-        _addr(q), _addr(k), _addr(v), _addr(log_a), _addr(s0), _addr(out), _addr(sn), _addr(starts), int(B), int(n), int(H),
-        int(H if Hk is None else Hk), int(K), int(V), int(q_stride), int(k_stride), int(v_stride), scale, int(flags), _stream_handle(stream)))
+    if Hk is None:
+        Hk = H
+    st = (_call or _native()).linear_attention(q, k, v, log_a, s0, out, sn, starts, B, n, H, Hk, K, V, q_stride, k_stride, v_stride, scale,
+                                               flags, stream)
+    if st is NotImplemented:
+        st = _convert_operator(_lib.heinsen_linear_attention, (q, k, v, log_a, s0, out, sn, starts),
+                               (B, n, H, Hk, K, V, q_stride, k_stride, v_stride), scale, flags, stream)
+    if st != HEINSEN_OK:
+        _raise_for(st)
 
 
 def heinsen_linear_attention_backward(q, k, v, log_a, s0, grad_out, grad_sn, grad_q, grad_k, grad_v, grad_log_a, grad_s0, B: int, n: int,
                                       H: int, K: int, V: int, scale: float, flags: int, stream=None, *, Hk=None, starts=None,
                                       q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> None:
     """Gradients of heinsen_linear_attention; see include/heinsen.h.  grad_sn, grad_log_a and grad_s0 may be None."""
-    _raise_for(load().heinsen_linear_attention_backward(
-        _addr(q), _addr(k), _addr(v), _addr(log_a), _addr(s0), _addr(grad_out), _addr(grad_sn), _addr(grad_q), _addr(grad_k), _addr(grad_v),
-        _addr(grad_log_a), _addr(grad_s0), _addr(starts), int(B), int(n), int(H), int(H if Hk is None else Hk), int(K), int(V),
-        int(q_stride), int(k_stride), int(v_stride), scale, int(flags), _stream_handle(stream)))
+    if Hk is None:
+        Hk = H
+    st = (_call or _native()).linear_attention_backward(q, k, v, log_a, s0, grad_out, grad_sn, grad_q, grad_k, grad_v, grad_log_a, grad_s0,
+                                                        starts, B, n, H, Hk, K, V, q_stride, k_stride, v_stride, scale, flags, stream)
+    if st is NotImplemented:
+        st = _convert_operator(_lib.heinsen_linear_attention_backward,
+                               (q, k, v, log_a, s0, grad_out, grad_sn, grad_q, grad_k, grad_v, grad_log_a, grad_s0, starts),
+                               (B, n, H, Hk, K, V, q_stride, k_stride, v_stride), scale, flags, stream)
+    if st != HEINSEN_OK:
+        _raise_for(st)
 
 
 def heinsen_block_norm(u, gate, residual, scale, w_post, w_pre, h, y, rows: int, D: int, eps: float, flags: int, stream=None, *,
                        u_stride: int = 0, gate_stride: int = 0) -> None:
     """h = residual + scale * act(gate) * norm(u) w_post, y = norm(h) w_pre; see include/heinsen.h.  Arguments that are not
     wanted are None."""
-    _raise_for(load().heinsen_block_norm(
-        _addr(u), _addr(gate), _addr(residual), _addr(scale), _addr(w_post), _addr(w_pre), _addr(h), _addr(y), int(rows), int(D),
-        int(u_stride), int(gate_stride), eps, int(flags), _stream_handle(stream)))
+    st = (_call or _native()).block_norm(u, gate, residual, scale, w_post, w_pre, h, y, rows, D, u_stride, gate_stride, eps, flags, stream)
+    if st is NotImplemented:
+        st = _convert_operator(_lib.heinsen_block_norm, (u, gate, residual, scale, w_post, w_pre, h, y), (rows, D, u_stride, gate_stride), eps,
+                               flags, stream)
+    if st != HEINSEN_OK:
+        _raise_for(st)
 
 
 def heinsen_block_norm_backward(u, gate, residual, scale, w_post, w_pre, grad_h, grad_y, grad_u, grad_gate, grad_residual, grad_scale,
                                 grad_w_post, grad_w_pre, rows: int, D: int, eps: float, flags: int, stream=None, *, u_stride: int = 0,
                                 gate_stride: int = 0) -> None:
     """Gradients of heinsen_block_norm; see include/heinsen.h.  All gradients but grad_u may be None."""
-    _raise_for(load().heinsen_block_norm_backward(
-        _addr(u), _addr(gate), _addr(residual), _addr(scale), _addr(w_post), _addr(w_pre), _addr(grad_h), _addr(grad_y), _addr(grad_u),
-        _addr(grad_gate), _addr(grad_residual), _addr(grad_scale), _addr(grad_w_post), _addr(grad_w_pre), int(rows), int(D), int(u_stride),
-        int(gate_stride), eps, int(flags), _stream_handle(stream)))
+    st = (_call or _native()).block_norm_backward(u, gate, residual, scale, w_post, w_pre, grad_h, grad_y, grad_u, grad_gate, grad_residual,
+                                                  grad_scale, grad_w_post, grad_w_pre, rows, D, u_stride, gate_stride, eps, flags, stream)
+    if st is NotImplemented:
+        st = _convert_operator(_lib.heinsen_block_norm_backward,
+                               (u, gate, residual, scale, w_post, w_pre, grad_h, grad_y, grad_u, grad_gate, grad_residual, grad_scale,
+                                grad_w_post, grad_w_pre), (rows, D, u_stride, gate_stride), eps, flags, stream)
+    if st != HEINSEN_OK:
+        _raise_for(st)

@@ -1,6 +1,7 @@
 """CPU-only checks of the operators for language models: what their entry points refuse, on the host and before any GPU work."""
 import math
 
+import numpy as np
 import pytest
 
 from paper_2311_06281_amd import binding as hb
@@ -79,3 +80,34 @@ def test_block_norm_backward_refuses(change, status):
 def test_the_scan_refuses_the_operators_flags():
     for flag in (hb.HEINSEN_DECAY_PER_HEAD, hb.HEINSEN_GATE_SIGMOID):
         assert hb.heinsen_scan_status(P, P, P, P, 1, 1, 8, 0, flag) == INVALID
+
+
+class _Tensor:
+    def __init__(self, at):
+        self.at = at
+
+    def data_ptr(self):
+        return self.at
+
+
+class _Stream:
+    cuda_stream = 0
+
+
+# tensors or addresses, numbers or what converts to them: one argument that is refused shows that each arrives in its place
+@pytest.mark.parametrize("direct", [True, False])
+@pytest.mark.parametrize("call,arguments,bad", [(hb.heinsen_linear_attention, ATTENTION, BAD_ATTENTION), (hb.heinsen_linear_attention_backward, BACKWARD, BAD_ATTENTION),
+                                                (hb.heinsen_block_norm, NORM, BAD_NORM), (hb.heinsen_block_norm_backward, NORM_BACKWARD, BAD_NORM)])
+def test_arguments_of_every_kind(monkeypatch, call, arguments, bad, direct):
+    hb.load()
+    if not direct:
+        monkeypatch.setattr(hb, "_call", hb._Converted)
+    counts = {"B", "n", "H", "K", "V", "Hk", "rows", "D", "flags"} | {m + "_stride" for m in ("q", "k", "v", "u", "gate")}
+    plain = {"scale", "eps", "starts"} if "K" in arguments else {"eps"}
+    for change, status in bad:
+        whole = arguments | change
+        tensors = {m: x if m in counts | plain or x is None else _Tensor(x) for m, x in whole.items()}
+        refused(status, call, **tensors, stream=_Stream())
+        refused(status, call, **{m: np.int64(x) if m in counts else x for m, x in whole.items()}, stream=0)
+    with pytest.raises(TypeError):
+        call(**(arguments | {"q" if "q" in arguments else "u": object()}))
