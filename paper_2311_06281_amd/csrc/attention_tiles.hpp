@@ -296,11 +296,13 @@ template <typename L, int C, int THREADS, bool NARROW> struct TileLoad {
     }
 };
 
-// four entries of a row of d float32 from `col` on, zeros after its end
-__device__ static inline f32x4 load4(const float *row, int col, int d)
+// Four entries of a row of d float32 from `col` on, zeros after its end.  ONCE: past the caches, which are left to what is read
+// again.
+template <bool ONCE = false> __device__ static inline f32x4 load4(const float *row, int col, int d)
 {
     f32x4 v = {0, 0, 0, 0};
-    if (col + 4 <= d) v = *reinterpret_cast<const Unaligned<float>::vec4 *>(row + col);
+    const auto *const whole = reinterpret_cast<const Unaligned<float>::vec4 *>(row + col);
+    if (col + 4 <= d) v = ONCE ? __builtin_nontemporal_load(whole) : *whole;
     else
 #pragma unroll
         for (int i = 0; i < 3; ++i)
@@ -308,13 +310,15 @@ __device__ static inline f32x4 load4(const float *row, int col, int d)
     return v;
 }
 
-// four entries of a row of d entries from `col` on; the row starts `row` entries behind `base`, the same in all lanes
-template <typename T> __device__ static inline void store4(T *base, uint32_t row, int col, int d, f32x4 v)
+// four entries of a row of d entries from `col` on; the row starts `row` entries behind `base`
+template <typename T, bool ONCE = false> __device__ static inline void store4(T *base, uint32_t row, int col, int d, f32x4 v)
 {
     char AS_GLOBAL *const to = (char AS_GLOBAL *)(uintptr_t)base;
     const uint32_t offset = (row + (uint32_t)col) * (uint32_t)sizeof(T);
     const x4<T> e = __builtin_convertvector(v, x4<T>);
-    if (col + 4 <= d) *(typename Unaligned<T>::vec4 AS_GLOBAL *)(to + offset) = e;
+    auto *const whole = (typename Unaligned<T>::vec4 AS_GLOBAL *)(to + offset);
+    if (col + 4 <= d && ONCE) __builtin_nontemporal_store(e, whole);
+    else if (col + 4 <= d) *whole = e;
     else
 #pragma unroll
         for (int i = 0; i < 3; ++i)
