@@ -11,7 +11,7 @@
 namespace hs {
 namespace {
 
-enum Sweep { kOutput, kSegmentState, kSegmentGradient, kChunkStates };
+enum Sweep { kOutput, kSegment, kChunkStates };
 
 struct SweepArgs {
     const void *q, *k, *v, *log_a;
@@ -22,12 +22,13 @@ struct SweepArgs {
     float *sn;
     int64_t n, q_stride, k_stride, v_stride;
     int64_t segment;         // tokens of a segment, a whole number of chunks
-    float *segment_state;    // [B, H, segments, K, V]: kSegment...: written; else, where there are several: the state at its start
-    float *segment_decay;    // [B, H, segments]: written by kSegment...
+    float *segment_state;    // [B, H, segments, K, V]: kSegment: written; else, where there are several: the state at its start
+    float *segment_decay;    // [B, H, segments]: written by kSegment
     int H, share, K, V, segments, chunks;
     int units;               // heads and segments of all sequences, a workgroup to each
     float scale;
     bool per_head;
+    bool back;               // kSegment: from the last chunk to the first
 };
 
 // The fragment with zeros in the place of infinite and NaN entries.
@@ -41,13 +42,12 @@ template <typename F> __device__ static inline F finite(F f)
 
 // A workgroup takes one segment of one head's tokens and goes through its chunks, the state in registers, sixteen columns to a
 // wave.  The heads' first segments come first, then their second ones and so on, so that ragged sequences leave no die idle.
-// kSegmentGradient goes from the last chunk to the first over (scale q, grad_out) in place of
-// (k, v) and gives the segment's own part of the gradient of the state it starts from.
-template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW, bool ROOMY>
-__global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep(SweepArgs p)
+// kSegment gives the segment's own part of the state at its end.  With `back` it goes from the last chunk to the first over
+// (scale q, grad_out) in place of (k, v) and gives the segment's own part of the gradient of the state it starts from.
+template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW, bool ROOMY> __device__ static inline void sweep_segment(const SweepArgs &p, int block)
 {
     constexpr int WAVES = DV / 16, THREADS = 64 * WAVES, KT = DK / 16, TT = C / 16;
-    constexpr bool BACK = SWEEP == kSegmentGradient;
+    const bool back = SWEEP == kSegment && p.back;
     constexpr bool FEW = sizeof(T) == 2 && DK == 128 && !ROOMY && (SWEEP == kOutput || DV == 64); // registers to keep addresses in
     typedef Tile<T, DK> LK;
     typedef Tile<T, DV> LV;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
     __shared__ int not_finite[2]; // of even and odd chunks
 
     const int lane0 = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), r = lane0 & 15, g = lane0 >> 4;
-    const int heads = gridDim.x / p.segments, seg = blockIdx.x / heads, bh = blockIdx.x % heads, h = bh % p.H, b = bh / p.H;
+    const int heads = p.units / p.segments, seg = block / heads, bh = block % heads, h = bh % p.H, b = bh / p.H;
     int64_t first;
     const int64_t len = uniform_sequence(p.starts, p.n, b, first);
     const int64_t begin = seg * p.segment, end = begin + p.segment < len ? begin + p.segment : len;
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
     double total = 0.0; // log2 of the decay so far (wave 0)
 
     const int chunks = (int)((end - begin + C - 1) / C);
-    auto chunk_start = [&](int i) { return begin + (int64_t)(BACK ? chunks - 1 - i : i) * C; };
+    auto chunk_start = [&](int i) { return begin + (int64_t)(back ? chunks - 1 - i : i) * C; };
     TileLoad<LK, C, THREADS, NARROW> next_q, next_k;
     TileLoad<LV, C, THREADS, NARROW> next_v;
     T next_log_a = (T)0.0f;
@@ -102,9 +102,9 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
         const int rows = (int)(end - t0 < C ? end - t0 : C);
         const uint32_t thread = (uint32_t)(64 * wave + fresh(lane0));
         next_k.load(rows, thread);
-        next_k.move(BACK ? -C : C);
+        next_k.move(back ? -C : C);
         next_v.load(rows, thread);
-        next_v.move(BACK ? -C : C);
+        next_v.move(back ? -C : C);
         if (SWEEP == kOutput) {
             next_q.load(rows, thread);
             next_q.move(C);
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
         if (next_v.not_finite() || odd) atomicOr(&not_finite[chunk & 1], 1);
         if (wave == 0) {
             const double chunk_total = write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
-            if (SWEEP == kSegmentState || BACK) total += chunk_total;
+            if (SWEEP == kSegment) total += chunk_total;
         }
         __syncthreads();
         const bool odd_values = not_finite[chunk & 1] != 0;
@@ -249,8 +249,8 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
         const int lane = FEW ? fresh(lane0) : lane0;
 #pragma unroll
         for (int i = 0; i < C / 32; ++i) {
-            f32x8 w = load_steps<T>((BACK ? decays.from_start : decays.to_end) + 32 * i, lane >> 4);
-            if (BACK) w *= p.scale;
+            f32x8 w = load_steps<T>((back ? decays.from_start : decays.to_end) + 32 * i, lane >> 4);
+            if (back) w *= p.scale;
             // v scaled by its decay enters unrounded
             Split<T> vw;
             vw.set(widen(vf[i]) * w, odd_values);
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
 
     const int row0 = fresh(4 * g), col0 = fresh(col);
     float *to = nullptr;
-    if (SWEEP == kSegmentState || SWEEP == kSegmentGradient) {
+    if (SWEEP == kSegment) {
         to = p.segment_state + ((int64_t)bh * p.segments + seg) * p.K * p.V;
         if (threadIdx.x == 0) p.segment_decay[(int64_t)bh * p.segments + seg] = __builtin_amdgcn_exp2f((float)total);
     } else if (SWEEP == kOutput && p.sn && end == len) {
@@ -297,32 +297,59 @@ __global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep
             }
 }
 
-// Chains the segments: each one's own sum is replaced by the state it starts from (BACK: the gradient it ends with).
-template <bool BACK>
-__global__ __launch_bounds__(256) void heinsen_attention_chain(float *segment_state, const float *segment_decay, const float *init,
-                                                               const int64_t *starts, int64_t n, int64_t segment, int H, int segments,
-                                                               int size)
+template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW, bool ROOMY>
+__global__ __launch_bounds__(4 * DV, ROOMY ? 2 : 4) void heinsen_attention_sweep(SweepArgs p)
 {
-    const int blocks = (size + 255) / 256, bh = blockIdx.x / blocks, at = blockIdx.x % blocks * 256 + threadIdx.x;
-    int64_t first;
-    const int64_t len = uniform_sequence(starts, n, bh / H, first);
+    sweep_segment<T, C, DK, DV, SWEEP, NARROW, ROOMY>(p, blockIdx.x);
+}
+
+struct TwoSweeps {
+    SweepArgs of[2]; // of as many units
+};
+
+// Two sweeps side by side: with one segment to a compute unit each alone has half the waves that hide one another's waits (64
+// heads of 4096 tokens in four segments, bfloat16: 92 us one after the other, 71 like this).
+template <typename T, int C, int DK, int DV, bool NARROW>
+__global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_two_sweeps(TwoSweeps p)
+{
+    const int units = p.of[0].units, which = (int)blockIdx.x >= units;
+    sweep_segment<T, C, DK, DV, kSegment, NARROW, false>(p.of[which], blockIdx.x - which * units);
+}
+
+// Chains the segments: each one's own sum is replaced by the state it starts from (back: the gradient it ends with).
+struct ChainArgs {
+    float *segment_state;
+    const float *segment_decay, *init;
+    bool back;
+};
+
+// `first` by the first half of the workgroups (or all), `second` by the others
+__global__ __launch_bounds__(256) void heinsen_attention_chain(ChainArgs first, ChainArgs second, const int64_t *starts, int64_t n, int64_t segment,
+                                                               int H, int heads, int segments, int size)
+{
+    const int blocks = (size + 255) / 256;
+    const bool other = blockIdx.x / blocks >= (uint32_t)heads;
+    const ChainArgs p = other ? second : first;
+    const int bh = blockIdx.x / blocks - (other ? heads : 0), at = blockIdx.x % blocks * 256 + threadIdx.x;
+    int64_t unused;
+    const int64_t len = uniform_sequence(starts, n, bh / H, unused);
     const int used = (int)((len + segment - 1) / segment);
     if (at >= size) return;
-    float s = init ? init[(int64_t)bh * size + at] : 0.0f;
+    float s = p.init ? p.init[(int64_t)bh * size + at] : 0.0f;
     constexpr int AHEAD = 8; // loads under way
     for (int i = 0; i < used; i += AHEAD) {
         float own[AHEAD], decay[AHEAD];
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) {
             const int last = used - 1, k = i + e < last ? i + e : last;
-            const int64_t j = (int64_t)bh * segments + (BACK ? last - k : k);
-            own[e] = segment_state[j * size + at];
-            decay[e] = segment_decay[j];
+            const int64_t j = (int64_t)bh * segments + (p.back ? last - k : k);
+            own[e] = p.segment_state[j * size + at];
+            decay[e] = p.segment_decay[j];
         }
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e)
             if (i + e < used) {
-                segment_state[((int64_t)bh * segments + (BACK ? used - 1 - i - e : i + e)) * size + at] = s;
+                p.segment_state[((int64_t)bh * segments + (p.back ? used - 1 - i - e : i + e)) * size + at] = s;
                 s = s * decay[e] + own[e];
             }
     }
@@ -415,24 +442,27 @@ __global__ __launch_bounds__(256) void heinsen_attention_step(StepArgs p)
 
 template <typename T> constexpr int chunk_tokens() { return sizeof(T) == 2 ? 64 : 32; }
 
-template <typename T, int SWEEP, int DK, int DV, bool NARROW, bool ROOMY = false> hipError_t sweep_sized(SweepArgs &a, hipStream_t stream)
+// second: null, or the sweep to do beside a kSegment one
+template <typename T, int SWEEP, int DK, int DV, bool NARROW, bool ROOMY = false> hipError_t sweep_sized(const SweepArgs &a, const SweepArgs *second, hipStream_t stream)
 {
-    heinsen_attention_sweep<T, chunk_tokens<T>(), DK, DV, SWEEP, NARROW, ROOMY><<<dim3((unsigned)a.units), 4 * DV, 0, stream>>>(a);
+    constexpr int C = chunk_tokens<T>();
+    if (second) heinsen_attention_two_sweeps<T, C, DK, DV, NARROW><<<dim3((unsigned)a.units * 2), 4 * DV, 0, stream>>>(TwoSweeps{{a, *second}});
+    else heinsen_attention_sweep<T, C, DK, DV, SWEEP, NARROW, ROOMY><<<dim3((unsigned)a.units), 4 * DV, 0, stream>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int SWEEP> hipError_t sweep(SweepArgs &a, hipStream_t stream)
+template <typename T, int SWEEP> hipError_t sweep(const SweepArgs &a, hipStream_t stream, const SweepArgs *second = nullptr)
 {
     constexpr int N = 16 / (int)sizeof(T);
     if (a.K < N || a.V < N) {
-        if (a.K > 64) return sweep_sized<T, SWEEP, 128, 64, true>(a, stream);
-        return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, true>(a, stream) : sweep_sized<T, SWEEP, 64, 128, true>(a, stream);
+        if (a.K > 64) return sweep_sized<T, SWEEP, 128, 64, true>(a, second, stream);
+        return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, true>(a, second, stream) : sweep_sized<T, SWEEP, 64, 128, true>(a, second, stream);
     }
-    if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, false>(a, stream) : sweep_sized<T, SWEEP, 64, 128, false>(a, stream);
-    if (a.V <= 64) return sweep_sized<T, SWEEP, 128, 64, false>(a, stream);
+    if (a.K <= 64) return a.V <= 64 ? sweep_sized<T, SWEEP, 64, 64, false>(a, second, stream) : sweep_sized<T, SWEEP, 64, 128, false>(a, second, stream);
+    if (a.V <= 64) return sweep_sized<T, SWEEP, 128, 64, false>(a, second, stream);
     // where there is one workgroup to a compute unit only, its waves can have all registers
-    if (SWEEP == kOutput && a.units < 2 * compute_units()) return sweep_sized<T, SWEEP, 128, 128, false, SWEEP == kOutput>(a, stream);
-    return sweep_sized<T, SWEEP, 128, 128, false>(a, stream);
+    if (SWEEP == kOutput && a.units < 2 * compute_units()) return sweep_sized<T, SWEEP, 128, 128, false, SWEEP == kOutput>(a, second, stream);
+    return sweep_sized<T, SWEEP, 128, 128, false>(a, second, stream);
 }
 
 SweepArgs sweep_args(const AttentionCall &c, const Segments &s)
@@ -443,15 +473,6 @@ SweepArgs sweep_args(const AttentionCall &c, const Segments &s)
     a.H = c.H, a.share = c.share, a.K = c.K, a.V = c.V, a.scale = c.scale, a.per_head = c.per_head;
     a.segment = s.tokens, a.segments = s.count, a.units = c.B * c.H * s.count;
     return a;
-}
-
-hipError_t chain(bool back, float *state, const float *decay, const float *init, const AttentionCall &c, const Segments &s)
-{
-    const int size = c.K * c.V;
-    const dim3 grid((unsigned)((size + 255) / 256 * c.B * c.H));
-    if (back) heinsen_attention_chain<true><<<grid, 256, 0, c.stream>>>(state, decay, init, c.starts, c.n, s.tokens, c.H, s.count, size);
-    else heinsen_attention_chain<false><<<grid, 256, 0, c.stream>>>(state, decay, init, c.starts, c.n, s.tokens, c.H, s.count, size);
-    return hipGetLastError();
 }
 
 template <typename T, int COLS> hipError_t step_sized(StepArgs &a, const AttentionCall &c)
@@ -501,22 +522,24 @@ size_t segment_scratch(const AttentionCall &c, const Segments &s)
     return align_up(count * c.K * c.V * sizeof(float), 256) + align_up(count * sizeof(float), 256);
 }
 
-// The states at the segments' starts (BACK: the gradients at their ends) from the segments' own sums.
-hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, bool back, void *scratch)
+// The states at the segments' starts and, in the second scratch if there is one, the gradients of those at their ends, from the
+// segments' own sums.
+hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, void *states, void *gradients)
 {
-    SweepArgs a = sweep_args(c, s);
-    a.segment_state = static_cast<float *>(scratch);
-    a.segment_decay = a.segment_state + align_up((size_t)c.B * c.H * s.count * c.K * c.V * sizeof(float), 256) / sizeof(float);
-    hipError_t e;
-    if (back) {
-        a.k = c.q, a.k_stride = c.q_stride;
-        a.v = c.grad_out, a.v_stride = (int64_t)c.H * c.V;
-        e = c.bf16 ? sweep<__bf16, kSegmentGradient>(a, c.stream) : sweep<float, kSegmentGradient>(a, c.stream);
-    } else {
-        e = c.bf16 ? sweep<__bf16, kSegmentState>(a, c.stream) : sweep<float, kSegmentState>(a, c.stream);
-    }
+    SweepArgs a = sweep_args(c, s), g = a;
+    const size_t decays = align_up((size_t)c.B * c.H * s.count * c.K * c.V * sizeof(float), 256) / sizeof(float);
+    a.segment_state = static_cast<float *>(states), a.segment_decay = a.segment_state + decays;
+    g.segment_state = static_cast<float *>(gradients), g.segment_decay = g.segment_state + decays;
+    g.k = c.q, g.k_stride = c.q_stride;
+    g.v = c.grad_out, g.v_stride = (int64_t)c.H * c.V;
+    g.back = true;
+    const hipError_t e = c.bf16 ? sweep<__bf16, kSegment>(a, c.stream, gradients ? &g : nullptr) : sweep<float, kSegment>(a, c.stream, gradients ? &g : nullptr);
     if (e != hipSuccess) return e;
-    return chain(back, a.segment_state, a.segment_decay, back ? c.grad_sn : c.s0, c, s);
+    const int size = c.K * c.V, heads = c.B * c.H;
+    const ChainArgs forward = {a.segment_state, a.segment_decay, c.s0, false}, backward = {g.segment_state, g.segment_decay, c.grad_sn, true};
+    heinsen_attention_chain<<<dim3((unsigned)((size + 255) / 256 * heads * (gradients ? 2 : 1))), 256, 0, c.stream>>>(forward, backward, c.starts, c.n, s.tokens,
+                                                                                                                    c.H, heads, s.count, size);
+    return hipGetLastError();
 }
 
 hipError_t attention_chunk_states(const AttentionCall &c, const Segments &s, float *segment_state, void *states, uint32_t *fine, int chunks)
@@ -536,7 +559,7 @@ hipError_t attention_launch(const AttentionCall &c, void *scratch)
     if (c.n <= kFewTokens) return c.bf16 ? step<__bf16>(c) : step<float>(c);
     const Segments s = attention_segments(c, false);
     if (s.count > 1) {
-        const hipError_t e = attention_segment_states(c, s, false, scratch);
+        const hipError_t e = attention_segment_states(c, s, scratch, nullptr);
         if (e != hipSuccess) return e;
     }
     SweepArgs a = sweep_args(c, s);

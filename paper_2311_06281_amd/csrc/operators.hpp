@@ -32,7 +32,7 @@ struct Segments {
 };
 Segments attention_segments(const AttentionCall &c, bool back);
 size_t segment_scratch(const AttentionCall &c, const Segments &s);
-hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, bool back, void *scratch);
+hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, void *states, void *gradients);
 hipError_t attention_chunk_states(const AttentionCall &c, const Segments &s, float *segment_state, void *states, uint32_t *fine, int chunks);
 constexpr int kFewTokens = 4; // sequences of up to so many go token by token
 int attention_chunk_tokens(bool bf16); // of the stored chunk states
