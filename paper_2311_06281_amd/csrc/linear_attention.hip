@@ -501,13 +501,15 @@ template <typename T> hipError_t step(const AttentionCall &c)
 //     128 heads, ragged lengths up to 4096        2: 236    4: 206    6: 175    8: 203
 //     4 heads of K = V = 48, float32, 131072      64: 338   128: 259  192: 245  256: 237
 //     64 heads, 4096, backward                    4: 459    8: 477
-//     60 heads of K = 55, V = 77, ragged up to 3001, backward    5: 187   6: 164
-// Of the backward pass two workgroups fit a compute unit at K, V <= 64 only.
+//     60 heads of K = 55, V = 77, ragged up to 3001, backward    5: 191   9: 144   18: 156
+// Of the backward pass two workgroups fit a compute unit at K, V <= 64 only.  A segment has four times the bytes of its state in
+// tokens at least: with half as much the fourth line takes 487, and with 512 tokens the fifth 164.
 Segments attention_segments(const AttentionCall &c, bool back)
 {
     const int64_t heads = (int64_t)c.B * c.H, per_unit = !back ? 3 : c.starts || (c.K <= 64 && c.V <= 64) ? 2 : 1, want = per_unit * compute_units();
     int64_t count = heads >= compute_units() ? 1 : (want + heads - 1) / heads;
-    const int64_t most = (c.n + 511) / 512;
+    const int64_t state = (int64_t)c.K * c.V * 4, token = (int64_t)(c.K + c.V) * (c.bf16 ? 2 : 4), least = (4 * state / token + 63) / 64 * 64;
+    const int64_t most = (c.n + least - 1) / least;
     if (count > most) count = most;
     Segments s;
     s.tokens = ((c.n + count - 1) / count + 63) / 64 * 64;
