@@ -247,6 +247,7 @@ int heinsen_test_carry(uint32_t spin_limit, uint32_t drop_tile, uint32_t epoch, 
  * stand around such a block.  Both are asynchronous on `stream`, take device pointers and return a heinsen_status_t
  * as heinsen_scan does; nothing is launched where arguments are refused.  With HEINSEN_IN_BF16 the arrays named
  * "stored" below are bfloat16, else float32.  Sums, states and statistics are float32 or wider throughout.
+ * Arrays that an argument's description does not call optional are never NULL, also where sequences have no tokens.
  * Workspace: a grow-only buffer per (device, stream) apart from the scan's, under the same rules: allocated by the first
  * call that needs it or needs more (HEINSEN_ERR_ALLOC), used as it is by a call recorded into a HIP graph
  * (HEINSEN_ERR_UNSUPPORTED where an ordinary call of at least the same shape has not been made on that stream), freed by
@@ -293,9 +294,9 @@ int heinsen_linear_attention(const void *q, const void *k, const void *v, const 
  *   grad_log_a : stored, [tokens, H], or [H] with HEINSEN_DECAY_PER_HEAD (the sum over all tokens); may be NULL.
  *   grad_s0    : [B, H, K, V] float32; may be NULL.
  * Nothing of the forward call is needed.  Workspace: the states at the chunks' starts (64 tokens in bfloat16, 32 in float32),
- * stored, K and V rounded up to 64 or 128, B * ceil(n / chunk) of them for each head; with shared heads 8 K more bytes for each
- * of B n H tokens and heads.  An infinite or NaN value reaches the gradients of its own sequence and head only, those
- * of earlier tokens among them.
+ * stored (in bfloat16 with eight more bits), K and V rounded up to 64 or 128, B * ceil(n / chunk) of them for each head; two sums
+ * for each segment as above; with shared heads 8 K more bytes for each of B n H tokens and heads.  An infinite or NaN value
+ * reaches the gradients of its own sequence and head only, those of earlier tokens among them.
  */
 int heinsen_linear_attention_backward(const void *q, const void *k, const void *v, const void *log_a, const void *s0,
                                       const void *grad_out, const void *grad_sn, void *grad_q, void *grad_k, void *grad_v,
