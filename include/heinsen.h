@@ -273,6 +273,7 @@ int heinsen_test_carry(uint32_t spin_limit, uint32_t drop_tile, uint32_t epoch, 
  *              starts[b] .. starts[b + 1] - 1, and n is at least the length of the longest one (tokens past the n-th of a
  *              sequence are left out).  A sequence without tokens hands its state on.
  *   K, V     : 1 .. 128 (HEINSEN_ERR_UNSUPPORTED above).  Wider values are several heads that share q, k and log_a.
+ *   Strides, H V and, for gradients of shared heads, H K are at most 2^23 elements (HEINSEN_ERR_UNSUPPORTED).
  *
  * Single tokens of a generating model are n = 1 with sn = s0.  n <= 4 goes token by token, which reads and writes the states
  * once and little else; longer sequences go in chunks, those of few heads in segments side by side (workspace:

@@ -188,6 +188,7 @@ int heinsen_linear_attention_backward(const void *q, const void *k, const void *
     if (!grad_out || !grad_q || !grad_k || !grad_v || (grad_log_a && !log_a)) return HEINSEN_ERR_INVALID_ARG;
     if (!hs::aligned({grad_out, grad_q, grad_k, grad_v, grad_log_a}, c.bf16 ? 2 : 4) || !hs::aligned({grad_sn, grad_s0}, 4))
         return HEINSEN_ERR_INVALID_ARG;
+    if (c.share > 1 && H * K > ((int64_t)1 << 23)) return HEINSEN_ERR_UNSUPPORTED; // rows of the heads' own gradients, as above
     c.grad_out = grad_out;
     c.grad_sn = static_cast<const float *>(grad_sn);
     c.grad_q = grad_q, c.grad_k = grad_k, c.grad_v = grad_v, c.grad_log_a = grad_log_a;

@@ -77,6 +77,12 @@ def test_block_norm_backward_refuses(change, status):
     refused(status, hb.heinsen_block_norm_backward, **(NORM_BACKWARD | change))
 
 
+# a token's gradients of its own heads' q and k, which are added up afterwards, have to lie within 32 bits for a chunk of tokens
+def test_attention_backward_refuses_too_many_shared_heads():
+    shared = BACKWARD | dict(H=1 << 17, Hk=1 << 10, K=128, V=1)
+    refused(UNSUPPORTED, hb.heinsen_linear_attention_backward, **shared)
+
+
 def test_the_scan_refuses_the_operators_flags():
     for flag in (hb.HEINSEN_DECAY_PER_HEAD, hb.HEINSEN_GATE_SIGMOID):
         assert hb.heinsen_scan_status(P, P, P, P, 1, 1, 8, 0, flag) == INVALID
