@@ -17,8 +17,9 @@ struct SweepArgs {
     const void *q, *k, *v, *log_a;
     const float *s0;
     const int64_t *starts;
-    void *out;               // kOutput: out; kChunkStates: the state at each chunk's start, transposed, [B, H, chunks, DV, DK] in T
-    uint32_t *fine;          // kChunkStates in bfloat16: [B, H, chunks, waves, 64, DK / 16], more bits of these states
+    void *out;               // kOutput: out; kChunkStates: the state at each chunk's start, [B, H, chunks] times: float32 transposed, [DV, DK];
+                             // bfloat16 in the order of the waves' registers, [DK / 32, waves, 64, 8]
+    uint32_t *fine;          // kChunkStates in bfloat16: [B, H, chunks, DK / 64, waves, 64, 4], more bits of these states
     float *sn;
     int64_t n, q_stride, k_stride, v_stride;
     int64_t segment;         // tokens of a segment, a whole number of chunks
@@ -186,15 +187,21 @@ template <typename T, int C, int DK, int DV, int SWEEP, bool NARROW, bool ROOMY>
         }
         if (SWEEP == kChunkStates) {
             T *const to = static_cast<T *>(p.out) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV);
-            const uint32_t at = (uint32_t)fresh(col * DK + 4 * g);
-#pragma unroll
-            for (int i = 0; i < KT; ++i)
-                *reinterpret_cast<x4<T> *>(to + at + 16 * i) = __builtin_convertvector(state[i], x4<T>);
             if (sizeof(T) == 2) {
-                uint32_t *const fine = p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4) + (uint32_t)fresh((64 * wave + lane0) * KT);
+                const uint32_t at = (uint32_t)fresh(64 * wave + lane0); // in 16 bytes, and so all lanes' of a store are side by side
+                uint32_t *const fine = p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4);
+#pragma unroll
+                for (int i = 0; i < KT; i += 2)
+                    *reinterpret_cast<Frag<T> *>(to + (at + i / 2 * THREADS) * 8) =
+                        join<T>(__builtin_convertvector(state[i], x4<T>), __builtin_convertvector(state[i + 1], x4<T>));
 #pragma unroll
                 for (int i = 0; i < KT; i += 4)
-                    *reinterpret_cast<u32x4 *>(fine + i) = u32x4{fine_bits(state[i]), fine_bits(state[i + 1]), fine_bits(state[i + 2]), fine_bits(state[i + 3])};
+                    *reinterpret_cast<u32x4 *>(fine + (at + i / 4 * THREADS) * 4) =
+                        u32x4{fine_bits(state[i]), fine_bits(state[i + 1]), fine_bits(state[i + 2]), fine_bits(state[i + 3])};
+            } else {
+                const uint32_t at = (uint32_t)fresh(col * DK + 4 * g);
+#pragma unroll
+                for (int i = 0; i < KT; ++i) *reinterpret_cast<x4<T> *>(to + at + 16 * i) = __builtin_convertvector(state[i], x4<T>);
             }
         }
 

@@ -22,8 +22,8 @@ struct BackwardArgs {
     const void *q, *k, *v, *log_a, *grad_out;
     const float *grad_sn;
     const int64_t *starts;
-    const void *states;           // [B, H, chunks, DV, DK] in T: the state at each chunk's start, transposed
-    const uint32_t *fine;         // bfloat16: [B, H, chunks, waves, 64, DK / 16] more bits of these states, in the order of a wave's registers
+    const void *states;           // the state at each chunk's start, as the sweep over chunks leaves it
+    const uint32_t *fine;         // bfloat16: more bits of these states
     const float *segment_grad;    // [B, H, segments, K, V]: where there are several, the gradient of the state at each one's end
     void *grad_q, *grad_k;        // T, or float for each head of v where heads share q and k
     void *grad_v, *grad_log_a;    // grad_log_a: T, or float [tokens, H] with per_head, or null
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     const int chunks = (int)((end - begin + C - 1) / C);
     TileLoad<LK, C, THREADS, NARROW> next_q, next_k;
     TileLoad<LV, C, THREADS, NARROW> next_v, next_o;
-    TileLoad<LK, STAGED ? DV : THREADS * 16 / (int)sizeof(T) / DK, THREADS, false> next_s;
+    Frag<T> next_s[STAGED ? KT / 2 : 1];
     T next_log_a = (T)0.0f;
     auto state_of = [&](int64_t t0) { return static_cast<const T *>(p.states) + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV); };
     const int64_t last = begin + (int64_t)(chunks - 1) * C; // the last chunk's first token
@@ -103,7 +103,6 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
     next_k.start(k + last * p.k_stride, p.k_stride, p.K);
     next_v.start(v + last * p.v_stride, p.v_stride, p.V);
     next_o.start(o + last * o_stride, o_stride, p.V);
-    if (STAGED) next_s.start(state_of(last), DK, DK);
     auto request = [&](int64_t t0) {
         const int rows = (int)(end - t0 < C ? end - t0 : C);
         const uint32_t thread = (uint32_t)(64 * wave + fresh(lane0));
@@ -115,10 +114,9 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         next_v.move(-C);
         next_o.load(rows, thread);
         next_o.move(-C);
-        if (STAGED) {
-            next_s.load(DV, thread);
-            next_s.move(-DV);
-        }
+        if (STAGED)
+#pragma unroll
+            for (int i = 0; i < KT / 2; ++i) next_s[i] = *reinterpret_cast<const Frag<T> *>(state_of(t0) + (thread + i * THREADS) * 8);
         if (log_a && wave == 0) next_log_a = log_a[p.per_head ? h : (first + t0 + fresh(lane0 < rows ? lane0 : 0)) * p.H + h];
     };
     if (chunks > 0) request(last);
@@ -134,7 +132,14 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         next_v.store(vs, v + t0 * p.v_stride, p.v_stride, rows, p.V);
         next_o.settle(p.V);
         next_o.store(os, o + t0 * o_stride, o_stride, rows, p.V);
-        if (STAGED) next_s.store(ss, state_of(t0), DK, DV, DK);
+        if (STAGED) {
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
+#pragma unroll
+            for (int i = 0; i < KT / 2; ++i) {
+                *reinterpret_cast<x4<T> *>(ss + LK::at(16 * wave, r, 32 * i, 4 * g)) = __builtin_shufflevector(next_s[i], next_s[i], 0, 1, 2, 3);
+                *reinterpret_cast<x4<T> *>(ss + LK::at(16 * wave, r, 32 * i + 16, 4 * g)) = __builtin_shufflevector(next_s[i], next_s[i], 4, 5, 6, 7);
+            }
+        }
         if (wave == 0) write_decays<C>(decays, lane0 < rows ? to_float(next_log_a) : 0.0f, lane0);
 #pragma unroll
         for (int i = 0; i < KT; ++i)
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
         if (STAGED)
 #pragma unroll
             for (int i = 0; i < KT / 4; ++i)
-                fine[i] = *reinterpret_cast<const u32x4 *>(p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4) + (uint32_t)fresh((64 * wave + lane0) * KT) + 4 * i);
+                fine[i] = *reinterpret_cast<const u32x4 *>(p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4) + (uint32_t)(64 * wave + fresh(lane0) + i * THREADS) * 4);
         if (chunk > 0) request(t0 - C);
 
         // P, D and the pairs' sums, in tiles of 16 x 16 on and below the diagonal, and zeros beside it where a product
