@@ -151,6 +151,18 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
             for (int i = 0; i < KT / 4; ++i)
                 fine[i] = *reinterpret_cast<const u32x4 *>(p.fine + ((int64_t)bh * p.chunks + t0 / C) * (DK * DV / 4) + (uint32_t)(64 * wave + fresh(lane0) + i * THREADS) * 4);
+        // float32: what the wave needs of the state is on its way while P and D are formed
+        Frag<T> early[STAGED ? 1 : DV / 32];
+        x4<T> span_of[STAGED ? 1 : KT];
+        if (!STAGED) {
+            const int lane = fresh(lane0), r = lane & 15, g = lane >> 4;
+#pragma unroll
+            for (int i = 0; i < DV / 32; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) early[i][e] = state[(32 * i + step_of<T>(g, e)) * DK + 16 * (wave % KT) + r];
+#pragma unroll
+            for (int i = 0; i < KT; ++i) span_of[i] = *reinterpret_cast<const x4<T> *>(state + (16 * wave + r) * DK + 16 * i + 4 * g);
+        }
         if (chunk > 0) request(t0 - C);
 
         // P, D and the pairs' sums, in tiles of 16 x 16 on and below the diagonal, and zeros beside it where a product
@@ -220,6 +232,7 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
             for (int i = 0; i < DV / 32; ++i) {
                 if (STAGED) sf[i] = load_cols<LK>(ss, 16 * kt, 32 * i, lane);
+                else if (WAVES >= KT || kt < WAVES) sf[i] = early[i];
                 else
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sf[i][e] = state[(32 * i + step_of<T>(g, e)) * DK + 16 * kt + r];
@@ -280,8 +293,8 @@ __global__ __launch_bounds__(4 * DV, 2) void heinsen_attention_backward(Backward
 #pragma unroll
             for (int i = 0; i < KT; ++i) {
                 f32x4 s;
-                if (STAGED) s = refined(*reinterpret_cast<const bf16x4 *>(ss + LK::at(16 * wave, r, 16 * i, 4 * g)), fine[i / 4][i % 4]);
-                else s = *reinterpret_cast<const f32x4 *>(state + col * DK + 16 * i + 4 * g);
+                if constexpr (STAGED) s = refined(*reinterpret_cast<const bf16x4 *>(ss + LK::at(16 * wave, r, 16 * i, 4 * g)), fine[i / 4][i % 4]);
+                else s = __builtin_convertvector(span_of[i], f32x4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += grad[i][e] * s[e];
                 grad[i] *= decay;
