@@ -251,6 +251,17 @@ def test_gradient_of_decays_over_long_sequences(hb, slow, bf16):
     run(hb, Case([1500], 1, 64, 64, bf16=bf16, slow=slow), "backward")
 
 
+# Of a long memory's decays nearly all of the gradient is <R, S> of states that are not rounded to bfloat16 for it: the result's own
+# rounding, 1.7e-3, and that of the terms within a chunk of 64 tokens, which are a part of it, at most as much again in the states
+# and their gradients over two thirds of it: sqrt(1.7^2 + 1.4^2) = 2.2e-3.  With states rounded once more it is 2.4e-3 and above.
+@pytest.mark.parametrize("slow", [1 / 32, 1 / 64])
+def test_gradient_of_slow_decays_is_rounded_once(hb, slow):
+    case = Case([1000], 6, 64, 96, slow=slow, seed=5)
+    _, _, grads = case.exact()
+    error, norm = check("log_a", case.backward(hb)["log_a"], grads["log_a"])
+    assert error <= 2.2e-3 * norm, error / norm
+
+
 # an infinite or NaN entry reaches its own sequence and head from its own token on, and nothing else
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
