@@ -48,8 +48,8 @@ template <typename F> __device__ static inline F finite(F f)
 // make its update and its outputs a matter of that wave alone; the weights of the tokens for one another are shared through LDS.
 // Bound by instructions: a SIMD unit's time is near four cycles a vector instruction and sixteen a matrix one, little of them at
 // once.  Measured, with bytes read and written once over time: 256 heads of 16384 tokens of 128 + 128 bfloat16 1.16 ms, 3.7 TB/s;
-// 64 heads of 4096 in segments 85 us of outputs, 45 of segments' states and 18 of their chain; 4 heads of 131072 tokens of 48 + 48
-// float32 156, 70 and 24 us.
+// 64 heads of 4096 in segments 85 us of outputs, 45 of segments' states and 14 of their chain; 4 heads of 131072 tokens of 48 + 48
+// float32 156, 70 and 15 us.
 //
 // kSegment gives the segment's own part of the state at its end.  With `back` it goes from the last chunk to the first over
 // (scale q, grad_out) in place of (k, v) and gives the segment's own part of the gradient of the state it starts from.
@@ -332,40 +332,45 @@ __global__ __launch_bounds__(4 * DV, 4) void heinsen_attention_two_sweeps(TwoSwe
 }
 
 // Chains the segments: each one's own sum is replaced by the state it starts from (back: the gradient it ends with).  Bound by
-// memory: 8 bytes an entry and segment, 128 heads of 128 x 128 in six segments 21 us.
+// memory: 8 bytes an entry and segment, 128 heads of 128 x 128 in six segments 12 us (21 with single entries to a thread).
 struct ChainArgs {
     float *segment_state;
     const float *segment_decay, *init;
     bool back;
 };
 
-// `first` by the first half of the workgroups (or all), `second` by the others
+// `first` by the first half of the workgroups (or all), `second` by the others.  A thread has VEC entries and AHEAD segments' of
+// them under way.
+template <int VEC, int AHEAD>
 __global__ __launch_bounds__(256) void heinsen_attention_chain(ChainArgs first, ChainArgs second, const int64_t *starts, int64_t n, int64_t segment,
                                                                int H, int heads, int segments, int size)
 {
-    const int blocks = (size + 255) / 256;
+    typedef float vec __attribute__((ext_vector_type(VEC), aligned(sizeof(float))));
+    const int blocks = (size + 256 * VEC - 1) / (256 * VEC);
     const bool other = blockIdx.x / blocks >= (uint32_t)heads;
     const ChainArgs p = other ? second : first;
-    const int bh = blockIdx.x / blocks - (other ? heads : 0), at = blockIdx.x % blocks * 256 + threadIdx.x;
+    const int bh = blockIdx.x / blocks - (other ? heads : 0), at = (blockIdx.x % blocks * 256 + threadIdx.x) * VEC;
     int64_t unused;
     const int64_t len = uniform_sequence(starts, n, bh / H, unused);
     const int used = (int)((len + segment - 1) / segment);
     if (at >= size) return;
-    float s = p.init ? p.init[(int64_t)bh * size + at] : 0.0f;
-    constexpr int AHEAD = 8; // loads under way
+    vec s = (vec)0.0f;
+    if (p.init) s = *reinterpret_cast<const vec *>(p.init + (int64_t)bh * size + at);
+    float *const state = p.segment_state + (int64_t)bh * segments * size + at;
+    const float *const decays = p.segment_decay + (int64_t)bh * segments;
     for (int i = 0; i < used; i += AHEAD) {
-        float own[AHEAD], decay[AHEAD];
+        vec own[AHEAD];
+        float decay[AHEAD];
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) {
-            const int last = used - 1, k = i + e < last ? i + e : last;
-            const int64_t j = (int64_t)bh * segments + (p.back ? last - k : k);
-            own[e] = p.segment_state[j * size + at];
-            decay[e] = p.segment_decay[j];
+            const int last = used - 1, k = i + e < last ? i + e : last, j = p.back ? last - k : k;
+            own[e] = *reinterpret_cast<const vec *>(state + (int64_t)j * size);
+            decay[e] = decays[j];
         }
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e)
             if (i + e < used) {
-                p.segment_state[((int64_t)bh * segments + (p.back ? used - 1 - i - e : i + e)) * size + at] = s;
+                *reinterpret_cast<vec *>(state + (int64_t)(p.back ? used - 1 - i - e : i + e) * size) = s;
                 s = s * decay[e] + own[e];
             }
     }
@@ -557,8 +562,13 @@ hipError_t attention_segment_states(const AttentionCall &c, const Segments &s, v
     if (e != hipSuccess) return e;
     const int size = c.K * c.V, heads = c.B * c.H;
     const ChainArgs forward = {a.segment_state, a.segment_decay, c.s0, false}, backward = {g.segment_state, g.segment_decay, c.grad_sn, true};
-    heinsen_attention_chain<<<dim3((unsigned)((size + 255) / 256 * heads * (gradients ? 2 : 1))), 256, 0, c.stream>>>(forward, backward, c.starts, c.n, s.tokens,
-                                                                                                                    c.H, heads, s.count, size);
+    // four entries to a thread where there are enough of them for all compute units (4 heads of 48 x 48, 192 segments: 21.8 us so,
+    // 15.2 with one)
+    const int vec = size % 4 == 0 && (int64_t)size * heads >= 1024 * compute_units() ? 4 : 1;
+    const dim3 grid((unsigned)((size + 256 * vec - 1) / (256 * vec) * heads * (gradients ? 2 : 1)));
+    const auto chain = vec == 4 ? (s.count > 8 ? heinsen_attention_chain<4, 32> : heinsen_attention_chain<4, 8>)
+                                : (s.count > 8 ? heinsen_attention_chain<1, 32> : heinsen_attention_chain<1, 8>);
+    chain<<<grid, 256, 0, c.stream>>>(forward, backward, c.starts, c.n, s.tokens, c.H, heads, s.count, size);
     return hipGetLastError();
 }
 

@@ -37,7 +37,7 @@ struct BackwardArgs {
 // All operands of a chunk are in LDS, 154 KB at K = V = 128 in bfloat16, so one workgroup of eight waves has a compute unit, two to a
 // SIMD unit; from counters its waves wait half of their time (for LDS, one another and results), vector instructions take 40 %
 // of a SIMD unit's, LDS 42 %, matrix products 12 %.  64 heads of 4096 tokens 265 us beside 82 for the chunks' first states, 71 for
-// segments and 18 for their chains: 436 us for 0.55 GB in and out and 0.4 GB of states between; float32, 128 heads of 4096 x (64 +
+// segments and 14 for their chains: 432 us for 0.55 GB in and out and 0.4 GB of states between; float32, 128 heads of 4096 x (64 +
 // 64) 466 us, of which matrix products are 44 %.  With sixteen waves of half the registers 305 us, with the sums of four tiles of
 // tokens side by side 263.
 //
